@@ -487,6 +487,87 @@ int bsp_linear_run(const bsp_linear_call* call, int route, int* route_taken, voi
 int bsp_linear_tune(const bsp_linear_call* call, int reps, int* best_route, float* ms_zero_expanded,
                     float* ms_gathered, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The linear layer in 8-bit floating point: serving and training the layer of Sections 3.1 / 4.4 and Algorithm 2 (W * Mask) with
+ * operands of half the bytes and twice the tensor-core rate of bf16.
+ *
+ * Form.  A value is e4m3 or e5m2 (`fmt`); 128 values share a scale that is a power of two, held as its exponent plus 127 in a
+ * byte: the smallest (at least 2^-127) that brings the largest magnitude to at most 448 (e4m3) or 57344 (e5m2).  Dividing by it is
+ * exact; the quotient is rounded to nearest, ties to even.  A block of zeros has scale byte 0.  A block that holds an infinity or a NaN is
+ * NaN throughout, under scale byte 127.
+ *   along rows     S[r, c / 128]: blocks of 128 columns of a row, the last one may be shorter.  S is uint8 [rows, ceil(cols / 128)], lds
+ *   along columns  Sc[r / 128, c]: blocks of 128 rows of a column.  Sc is uint8 [ceil(rows / 128), cols], ldsc
+ *   weight         S[r / 128, c / 128]: blocks of 128 x 128
+ * Values are uint8 matrices of X's shape with a leading dimension in bytes.
+ *
+ * bsp_fp8_quantize: X bf16 [rows, cols] (ldx) to 8 bits along its rows (Q, S: the operand of a product that sums over the
+ * columns) and / or along its columns (Qc, Sc: of one that sums over the rows) in one pass; a form whose pointers are NULL is
+ * left out.  col_sums (NULL: left out): float32 [cols], the sums of X's columns in float32, in a fixed order: with X = dY the
+ * bias gradient.  It needs ws, 4-byte aligned, of 4 * ceil(rows / 128) * cols bytes.
+ * bsp_fp8_quantize_weight: W bf16 [n_out, k_in] (ldw; bsp_linear_plan's execution layout, or W_bf16 of the Adam step) to e4m3 in
+ * the weight form.
+ *
+ * bsp_linear_fp8: Y = act(X (W * Mask)^T + bias) for bf16 X [tokens, k_in] (ldx), which is brought to e4m3 along its rows on the
+ * way; Wq, WS the weight form; bias bf16 [n_out] or NULL, act and the rounding of Y (bf16) as bsp_linear.  ws: device scratch of
+ * bsp_linear_fp8_ws_bytes bytes (host query), 16-byte aligned.
+ * bsp_linear_fp8_quantized: the same for activations that are in 8 bits already (Xq, XS along rows, of format fmt).
+ * bsp_linear_fp8_backward_input: dX = dY (W * Mask), dY along rows (dYq [tokens, n_out], dYS), Wq and WS as in the forward call;
+ * dX bf16 [tokens, k_in].
+ * bsp_linear_fp8_backward_weight: dW = (dY^T X) * Mask, both along columns (dYq [tokens, n_out], dYS [ceil(tokens / 128), n_out];
+ * Xq [tokens, k_in], XS [ceil(tokens / 128), k_in]); keep and block as in bsp_linear_backward_weight; dW bf16 [n_out, k_in].
+ *
+ * Products of 8-bit values are exact; they are added in float32 and the result is rounded to bf16 once.  8-bit matrices whose
+ * rows begin at multiples of 16 bytes go through the tensor cores, others through a slower CUDA-core kernel with the same semantics.
+ * Outputs may have any alignment; they are stored fastest where they are 16-byte aligned with rows and leading dimensions of a
+ * multiple of 8.  Bounded waits as bsp_linear_planned: check bsp_linear_status.
+ * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE (leading dimension too small, block does not divide n_out), BSP_ERR_WORKSPACE,
+ * BSP_ERR_UNSUPPORTED (bsp_fp8_quantize*: more than 65535 * 128 rows; bsp_linear_fp8*: more than 2^31 - 16 inputs). */
+typedef enum { BSP_FP8_E4M3 = 0, BSP_FP8_E5M2 = 1 } bsp_fp8_format;
+int bsp_fp8_quantize(const void* X, int rows, int cols, int ldx, int fmt, void* Q, int ldq, uint8_t* S, int lds, void* Qc, int ldqc,
+                     uint8_t* Sc, int ldsc, float* col_sums, void* ws, size_t ws_bytes, void* stream);
+int bsp_fp8_quantize_weight(const void* W, int n_out, int k_in, int ldw, void* Q, int ldq, uint8_t* S, int lds, void* stream);
+int bsp_linear_fp8_ws_bytes(int tokens, int k_in, size_t* bytes);
+int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* X, int tokens, int ldx,
+                   const void* bias, int act, void* Y, int ldy, void* ws, size_t ws_bytes, void* stream);
+int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* Xq, int ldx,
+                             const uint8_t* XS, int ldxs, int fmt, int tokens, const void* bias, int act, void* Y, int ldy, void* stream);
+int bsp_linear_fp8_backward_input(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* dYq, int ldy,
+                                  const uint8_t* dYS, int ldys, int fmt, int tokens, void* dX, int ldx, void* stream);
+int bsp_linear_fp8_backward_weight(const void* dYq, int ldy, const uint8_t* dYS, int ldys, int fmt_dy, const void* Xq, int ldx,
+                                   const uint8_t* XS, int ldxs, int fmt_x, int tokens, int n_out, int k_in, int block, const uint8_t* keep,
+                                   void* dW, int lddw, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * bsp_masked_adam_step_batched — bsp_masked_adam_step on many tensors in one launch per 96 of them, with moments of 32 or 8 bits
+ * and gradients in float32 or bf16.
+ *
+ * jobs: HOST array of n_jobs descriptors with device pointers.  W, W_bf16 (NULL: left out), keep (NULL: no mask), block, orient as in
+ * bsp_masked_adam_step; a bias is a tensor of one row.  lr and weight_decay (decoupled) are the tensor's own.  m and v have the leading
+ * dimension ldm.
+ *   state_bits 32: float32 moments.  Moments and, with the same step on the host, weights get the same bits as from bsp_masked_adam_step.
+ *   state_bits 8: m e4m3, v e5m2 (one byte each), m_scale and v_scale uint8 [rows, ceil(cols / 128)]: a power of two for each
+ *     128 neighbouring weights of a row, as in the form along rows above.  Zero bytes throughout are zero moments.  W is updated from the
+ *     new moments in float32; these are then rounded to one of their two neighbours with the distance as probability,
+ *     16 random bits each, a hash of (seed, step, number of the job in the array, position in the tensor): the same call
+ *     gives the same bits.  A positive v is never rounded to zero.  A block whose new moments hold an infinity or a NaN becomes NaN.
+ * grad_scale: device float that multiplies every gradient (clipping), or NULL.  step >= 1; if step_dev is not NULL the step is read from there
+ * instead, so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step.
+ * Any shape and alignment; 16-byte accesses where pointers and leading dimensions allow them.  No two jobs may share memory that either writes.
+ * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE, BSP_ERR_UNSUPPORTED (a tensor of more than 2^41 weights); all jobs are checked before the
+ * first launch. */
+typedef enum { BSP_GRAD_F32 = 0, BSP_GRAD_BF16 = 1 } bsp_grad_type;
+typedef struct bsp_adam_job {
+  float* W; int rows, cols, ldw;
+  const void* grad; int ldg; int grad_type;
+  void* m; void* v; int ldm; int state_bits;
+  uint8_t* m_scale; uint8_t* v_scale;
+  const uint8_t* keep; int block, orient;
+  float lr, weight_decay;
+  void* W_bf16; int ldb;
+} bsp_adam_job;
+int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs, float beta1, float beta2, float eps, int step, uint32_t seed,
+                                 const float* grad_scale, const int* step_dev, void* stream);
+
 /* bsp_linear_cuda_core — the same layer computed straight from the packed form by a plain
  * CUDA-core kernel (one thread per output, float32 accumulation in index order).  It is what
  * bsp_linear falls back to when the alignment rules above do not hold, and is exported so the

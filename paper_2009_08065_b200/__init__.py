@@ -14,6 +14,9 @@ from .binding import (  # noqa: F401
     LINEAR_AUTO, LINEAR_ONE_CTA, LINEAR_CTA_PAIR, LINEAR_PLAN_STABLE, LINEAR_OUT_TRANSPOSED, bsp_linear_gathered_ex, bsp_linear, bsp_linear_status, bsp_linear_chain, bsp_linear_chain_ws_bytes,
     bsp_linear_gather_plan_bytes, bsp_linear_gather_plan, bsp_transpose, bsp_linear_gathered,
     bsp_masked_adam_step, bsp_repack_values, bsp_dense_mask,
+    FP8_E4M3, FP8_E5M2, bsp_fp8_quantize, bsp_fp8_quantize_weight, bsp_linear_fp8_ws_bytes, bsp_linear_fp8, bsp_linear_fp8_quantized,
+    bsp_linear_fp8_backward_input, bsp_linear_fp8_backward_weight,
+    GRAD_F32, GRAD_BF16, AdamJob, make_adam_job_array, bsp_masked_adam_step_batched,
     bsp_linear_cuda_core, bsp_status_string, bsp_set_wait_limit_ms, bsp_wait_selftest,
     ROUTE_AUTO, ROUTE_ZERO_EXPANDED, ROUTE_GATHERED, make_linear_call, bsp_linear_route, bsp_linear_run, bsp_linear_tune,
 )

@@ -84,6 +84,19 @@ class _LinearCall(ctypes.Structure):
     ]
 
 
+class _AdamJob(ctypes.Structure):
+    """Mirror of `bsp_adam_job` in bsp.h."""
+    _fields_ = [
+        ("W", _vp), ("rows", _i), ("cols", _i), ("ldw", _i),
+        ("grad", _vp), ("ldg", _i), ("grad_type", _i),
+        ("m", _vp), ("v", _vp), ("ldm", _i), ("state_bits", _i),
+        ("m_scale", _vp), ("v_scale", _vp),
+        ("keep", _vp), ("block", _i), ("orient", _i),
+        ("lr", _f), ("weight_decay", _f),
+        ("W_bf16", _vp), ("ldb", _i),
+    ]
+
+
 _SIGNATURES = {
     "bsp_status_string": (ctypes.c_char_p, [_i]),
     "bsp_last_cuda_error": (_i, []),
@@ -121,6 +134,14 @@ _SIGNATURES = {
     "bsp_linear_status": (_i, [_vp]),
     "bsp_set_wait_limit_ms": (_i, [_i]),
     "bsp_wait_selftest": (_i, [ctypes.POINTER(_i), ctypes.POINTER(ctypes.c_longlong), _vp]),
+    "bsp_fp8_quantize": (_i, [_vp, _i, _i, _i, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _sz, _vp]),
+    "bsp_fp8_quantize_weight": (_i, [_vp, _i, _i, _i, _vp, _i, _vp, _i, _vp]),
+    "bsp_linear_fp8_ws_bytes": (_i, [_i, _i, _szp]),
+    "bsp_linear_fp8": (_i, [_vp, _i, _vp, _i, _i, _i, _vp, _i, _i, _vp, _i, _vp, _i, _vp, _sz, _vp]),
+    "bsp_linear_fp8_quantized": (_i, [_vp, _i, _vp, _i, _i, _i, _vp, _i, _vp, _i, _i, _i, _vp, _i, _vp, _i, _vp]),
+    "bsp_linear_fp8_backward_input": (_i, [_vp, _i, _vp, _i, _i, _i, _vp, _i, _vp, _i, _i, _i, _vp, _i, _vp]),
+    "bsp_linear_fp8_backward_weight": (_i, [_vp, _i, _vp, _i, _i, _vp, _i, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _i, _vp]),
+    "bsp_masked_adam_step_batched": (_i, [ctypes.POINTER(_AdamJob), _i, _f, _f, _f, _i, ctypes.c_uint32, _vp, _vp, _vp]),
     "bsp_linear_cuda_core": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _i, _i, _vp, _i, _vp, _i, _vp]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -364,6 +385,114 @@ def bsp_dense_mask(W: torch.Tensor, mask: torch.Tensor, stream=None) -> None:
 def bsp_repack_values(W: torch.Tensor, packed: PackedMatrix, stream=None) -> None:
     """Refreshes packed.vals from an updated bf16 W; blk_ptr and idx stay as they are."""
     _check(_native.repack_values(W, packed.block, packed.blk_ptr, packed.idx, packed.vals, stream), "bsp_repack_values")
+
+
+FP8_E4M3, FP8_E5M2 = 0, 1
+
+
+def bsp_fp8_quantize(X: torch.Tensor, fmt: int, Q: Optional[torch.Tensor] = None, S: Optional[torch.Tensor] = None,
+                     Qc: Optional[torch.Tensor] = None, Sc: Optional[torch.Tensor] = None,
+                     col_sums: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """X bf16 [rows, cols] to 8 bits along its rows (Q, S [rows, ceil(cols / 128)]) and / or its columns (Qc, Sc
+    [ceil(rows / 128), cols]); col_sums: float32 [cols], with ws of 4 * ceil(rows / 128) * cols bytes."""
+    _check(_native.fp8_quantize(X, fmt, Q, S, Qc, Sc, col_sums, ws, stream), "bsp_fp8_quantize")
+
+
+def bsp_fp8_quantize_weight(W: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, stream=None) -> None:
+    """W bf16 [n_out, k_in] to e4m3 with a scale for each block of 128 x 128 (S [ceil(n_out / 128), ceil(k_in / 128)])."""
+    _check(_native.fp8_quantize_weight(W, Q, S, stream), "bsp_fp8_quantize_weight")
+
+
+def bsp_linear_fp8_ws_bytes(tokens: int, k_in: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.bsp_linear_fp8_ws_bytes(tokens, k_in, ctypes.byref(n)), "bsp_linear_fp8_ws_bytes")
+    return n.value
+
+
+def bsp_linear_fp8(Wq: torch.Tensor, WS: torch.Tensor, X: torch.Tensor, bias: Optional[torch.Tensor], act: int,
+                   Y: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Y = act(X W^T + bias): Wq [n_out, k_in] and WS from bsp_fp8_quantize_weight, X bf16 [tokens, k_in]."""
+    _check(_native.linear_fp8(Wq, WS, X, bias, act, Y, ws, stream), "bsp_linear_fp8")
+
+
+def bsp_linear_fp8_quantized(Wq: torch.Tensor, WS: torch.Tensor, Xq: torch.Tensor, XS: torch.Tensor, fmt: int,
+                             bias: Optional[torch.Tensor], act: int, Y: torch.Tensor, stream=None) -> None:
+    """The same for activations that bsp_fp8_quantize has brought to 8 bits along their rows."""
+    _check(_native.linear_fp8_quantized(Wq, WS, Xq, XS, fmt, bias, act, Y, stream), "bsp_linear_fp8_quantized")
+
+
+def bsp_linear_fp8_backward_input(Wq: torch.Tensor, WS: torch.Tensor, dYq: torch.Tensor, dYS: torch.Tensor, fmt: int,
+                                  dX: torch.Tensor, stream=None) -> None:
+    """dX = dY W: dYq, dYS the output gradient in 8 bits along its rows."""
+    _check(_native.linear_fp8_backward_input(Wq, WS, dYq, dYS, fmt, dX, stream), "bsp_linear_fp8_backward_input")
+
+
+def bsp_linear_fp8_backward_weight(dYq: torch.Tensor, dYS: torch.Tensor, fmt_dy: int, Xq: torch.Tensor, XS: torch.Tensor,
+                                   fmt_x: int, block: int, keep: Optional[torch.Tensor], dW: torch.Tensor, stream=None) -> None:
+    """dW = (dY^T X) * Mask: both operands in 8 bits along their columns."""
+    _check(_native.linear_fp8_backward_weight(dYq, dYS, fmt_dy, Xq, XS, fmt_x, block, keep, dW, stream),
+           "bsp_linear_fp8_backward_weight")
+
+
+@dataclass
+class AdamJob:
+    """One tensor of a bsp_masked_adam_step_batched call: W float32 [rows, cols] (a bias: [1, cols]), grad float32 or bf16;
+    m, v float32, or 8-bit values (uint8 or torch's float8 types) with m_scale, v_scale uint8 [rows, ceil(cols / 128)]."""
+    W: torch.Tensor
+    grad: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    lr: float
+    weight_decay: float = 0.0
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    keep: Optional[torch.Tensor] = None
+    block: int = 1
+    orient: int = ORIENT_C
+    W_bf16: Optional[torch.Tensor] = None
+
+
+def make_adam_job_array(jobs):
+    """The host descriptor array for bsp_masked_adam_step_batched; build it once and reuse it while the tensors stay."""
+    arr = (_AdamJob * len(jobs))()
+    for a, j in zip(arr, jobs):
+        shape = tuple(j.W.shape)
+        for t in (j.grad, j.m, j.v, j.W_bf16):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"tensors of one job have shapes {shape} and {tuple(t.shape)}")
+        for t, size in ((j.W, 4), (j.m, j.v.element_size()), (j.W_bf16, 2)):
+            if t is not None and t.element_size() != size:
+                raise ValueError(f"unexpected element type {t.dtype}")
+        if j.m.element_size() not in (1, 4) or j.grad.element_size() not in (2, 4):
+            raise ValueError(f"unexpected element types {j.m.dtype}, {j.grad.dtype}")
+        if _ld(j.m) != _ld(j.v):
+            raise ValueError("m and v have different leading dimensions")
+        scales = (shape[0], (shape[1] + 127) // 128)
+        for t in (j.m_scale, j.v_scale):
+            if t is not None and (tuple(t.shape) != scales or not t.is_contiguous() or t.element_size() != 1):
+                raise ValueError(f"scales are contiguous bytes of shape {scales}")
+        a.W, a.rows, a.cols, a.ldw = _ptr(j.W), shape[0], shape[1], _ld(j.W)
+        a.grad, a.ldg, a.grad_type = _ptr(j.grad), _ld(j.grad), GRAD_BF16 if j.grad.element_size() == 2 else GRAD_F32
+        a.m, a.v, a.ldm, a.state_bits = _ptr(j.m), _ptr(j.v), _ld(j.m), 8 * j.m.element_size()
+        a.m_scale, a.v_scale = _ptr(j.m_scale), _ptr(j.v_scale)
+        a.keep, a.block, a.orient = _ptr(j.keep), j.block, j.orient
+        a.lr, a.weight_decay = j.lr, j.weight_decay
+        a.W_bf16, a.ldb = _ptr(j.W_bf16), 0 if j.W_bf16 is None else _ld(j.W_bf16)
+    return arr
+
+
+GRAD_F32, GRAD_BF16 = 0, 1
+
+
+def bsp_masked_adam_step_batched(jobs, beta1: float, beta2: float, eps: float, step: int, seed: int = 0,
+                                 grad_scale: Optional[torch.Tensor] = None, step_dev: Optional[torch.Tensor] = None,
+                                 stream=None) -> None:
+    """jobs: a list of AdamJob, or an array made by make_adam_job_array; grad_scale: one float32, step_dev: one int32, on the device."""
+    arr = jobs if isinstance(jobs, ctypes.Array) else make_adam_job_array(jobs)
+    if arr._type_ is not _AdamJob:
+        raise ctypes.ArgumentError(f"expected an array made by make_adam_job_array, got {type(jobs).__name__}")
+    _check(_native.masked_adam_step_batched(ctypes.addressof(arr), len(arr), beta1, beta2, eps, step, seed, grad_scale, step_dev,
+                                            stream), "bsp_masked_adam_step_batched")
 
 
 def bsp_linear_gather_plan_bytes(n_out: int, k_in: int, block: int) -> int:

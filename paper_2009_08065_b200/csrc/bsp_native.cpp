@@ -48,6 +48,26 @@ class Args {
     const int64_t ld = t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
     return Matrix{t.data_ptr(), static_cast<int>(t.size(0)), static_cast<int>(t.size(1)), static_cast<int>(ld)};
   }
+  static void want_shape(const Matrix& m, int rows, int cols) {
+    TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols, "expected a tensor of shape [", rows, ", ", cols, "], got [", m.rows, ", ", m.cols, "]");
+  }
+  void want_bytes(int i, size_t size) const {
+    TORCH_CHECK_VALUE(tensor(i).element_size() == static_cast<int64_t>(size), "expected elements of ", size, " bytes, got ", tensor(i).scalar_type());
+  }
+  // A contiguous tensor of `n` values.
+  void want_values(int i, long long n, size_t size) const {
+    TORCH_CHECK_VALUE(tensor(i).numel() == n && tensor(i).is_contiguous(), "expected a contiguous tensor of ", n, " values");
+    want_bytes(i, size);
+  }
+  // 8-bit values of a matrix of X's shape, and scale bytes of a given one; nothing for None.
+  Matrix matrix_like(int i, const Matrix& X) const { return scales(i, X.rows, X.cols); }
+  Matrix scales(int i, int rows, int cols) const {
+    if (a_[i] == Py_None) return Matrix{nullptr, 0, 0, 0};
+    const Matrix m = matrix(i);
+    want_shape(m, rows, cols);
+    want_bytes(i, 1);
+    return m;
+  }
   long long integer(int i) const {
     const long long v = PyLong_AsLongLong(a_[i]);
     if (v == -1 && PyErr_Occurred()) throw python_error();
@@ -92,6 +112,8 @@ PyObject* status_of(F call) {
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
+
+int blocks(int n) { return n > 0 ? (n - 1) / 128 + 1 : 0; }
 
 #define NATIVE(name) PyObject* name(PyObject*, PyObject* const* argv, Py_ssize_t argc)
 #define NATIVE_ARGS(name, want) HANDLE_TH_ERRORS const Args A(#name, argv, argc, want)
@@ -314,12 +336,141 @@ NATIVE(linear_run) {
   NATIVE_END
 }
 
+// (X, fmt, Q, S, Qc, Sc, col_sums, ws, stream)
+NATIVE(fp8_quantize) {
+  NATIVE_ARGS(fp8_quantize, 9);
+  const Matrix X = A.matrix(0), Q = A.matrix_like(2, X), S = A.scales(3, X.rows, blocks(X.cols));
+  const Matrix Qc = A.matrix_like(4, X), Sc = A.scales(5, blocks(X.rows), X.cols);
+  A.want_bytes(0, 2);
+  const int fmt = A.i32(1);
+  float* sums = A.ptr<float>(6);
+  if (sums != nullptr) A.want_values(6, X.cols, 4);
+  void* ws = A.ptr(7);
+  const size_t wsb = A.bytes(7);
+  void* s = A.stream(8);
+  return status_of([&] {
+    return bsp_fp8_quantize(X.p, X.rows, X.cols, X.ld, fmt, Q.p, Q.ld, static_cast<uint8_t*>(S.p), S.ld, Qc.p, Qc.ld, static_cast<uint8_t*>(Sc.p),
+                            Sc.ld, sums, ws, wsb, s);
+  });
+  NATIVE_END
+}
+
+// (W, Q, S, stream)
+NATIVE(fp8_quantize_weight) {
+  NATIVE_ARGS(fp8_quantize_weight, 4);
+  const Matrix W = A.matrix(0), Q = A.matrix_like(1, W), S = A.scales(2, blocks(W.rows), blocks(W.cols));
+  A.want_bytes(0, 2);
+  void* s = A.stream(3);
+  return status_of([&] { return bsp_fp8_quantize_weight(W.p, W.rows, W.cols, W.ld, Q.p, Q.ld, static_cast<uint8_t*>(S.p), S.ld, s); });
+  NATIVE_END
+}
+
+// (Wq, WS, X, bias, act, Y, ws, stream)
+NATIVE(linear_fp8) {
+  NATIVE_ARGS(linear_fp8, 8);
+  const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(5);
+  A.want_bytes(0, 1);
+  A.want_bytes(2, 2);
+  A.want_bytes(5, 2);
+  A.want_shape(X, X.rows, W.cols);
+  A.want_shape(Y, X.rows, W.rows);
+  const void* bias = A.ptr(3);
+  if (bias != nullptr) A.want_values(3, W.rows, 2);
+  const int act = A.i32(4);
+  void* ws = A.ptr(6);
+  const size_t wsb = A.bytes(6);
+  void* s = A.stream(7);
+  return status_of([&] {
+    return bsp_linear_fp8(W.p, W.ld, static_cast<uint8_t*>(WS.p), WS.ld, W.rows, W.cols, X.p, X.rows, X.ld, bias, act, Y.p, Y.ld, ws, wsb, s);
+  });
+  NATIVE_END
+}
+
+// (Wq, WS, Xq, XS, fmt, bias, act, Y, stream)
+NATIVE(linear_fp8_quantized) {
+  NATIVE_ARGS(linear_fp8_quantized, 9);
+  const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(7);
+  const Matrix XS = A.scales(3, X.rows, blocks(X.cols));
+  A.want_bytes(0, 1);
+  A.want_bytes(2, 1);
+  A.want_bytes(7, 2);
+  A.want_shape(X, X.rows, W.cols);
+  A.want_shape(Y, X.rows, W.rows);
+  const int fmt = A.i32(4), act = A.i32(6);
+  const void* bias = A.ptr(5);
+  if (bias != nullptr) A.want_values(5, W.rows, 2);
+  void* s = A.stream(8);
+  return status_of([&] {
+    return bsp_linear_fp8_quantized(W.p, W.ld, static_cast<uint8_t*>(WS.p), WS.ld, W.rows, W.cols, X.p, X.ld, static_cast<uint8_t*>(XS.p), XS.ld, fmt,
+                                    X.rows, bias, act, Y.p, Y.ld, s);
+  });
+  NATIVE_END
+}
+
+// (Wq, WS, dYq, dYS, fmt, dX, stream)
+NATIVE(linear_fp8_backward_input) {
+  NATIVE_ARGS(linear_fp8_backward_input, 7);
+  const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), dY = A.matrix(2), dX = A.matrix(5);
+  const Matrix dYS = A.scales(3, dY.rows, blocks(dY.cols));
+  A.want_bytes(0, 1);
+  A.want_bytes(2, 1);
+  A.want_bytes(5, 2);
+  A.want_shape(dY, dY.rows, W.rows);
+  A.want_shape(dX, dY.rows, W.cols);
+  const int fmt = A.i32(4);
+  void* s = A.stream(6);
+  return status_of([&] {
+    return bsp_linear_fp8_backward_input(W.p, W.ld, static_cast<uint8_t*>(WS.p), WS.ld, W.rows, W.cols, dY.p, dY.ld, static_cast<uint8_t*>(dYS.p), dYS.ld,
+                                         fmt, dY.rows, dX.p, dX.ld, s);
+  });
+  NATIVE_END
+}
+
+// (dYq, dYS, fmt_dy, Xq, XS, fmt_x, block, keep, dW, stream)
+NATIVE(linear_fp8_backward_weight) {
+  NATIVE_ARGS(linear_fp8_backward_weight, 10);
+  const Matrix dY = A.matrix(0), dYS = A.scales(1, blocks(dY.rows), dY.cols), X = A.matrix(3), XS = A.scales(4, blocks(X.rows), X.cols);
+  const Matrix dW = A.matrix(8);
+  A.want_bytes(0, 1);
+  A.want_bytes(3, 1);
+  A.want_bytes(8, 2);
+  A.want_shape(X, dY.rows, X.cols);
+  A.want_shape(dW, dY.cols, X.cols);
+  const int fmt_dy = A.i32(2), fmt_x = A.i32(5), block = A.i32(6);
+  const uint8_t* keep = A.ptr<uint8_t>(7);
+  if (keep != nullptr && block > 0) A.want_values(7, static_cast<long long>(dY.cols / block) * X.cols, 1);
+  void* s = A.stream(9);
+  return status_of([&] {
+    return bsp_linear_fp8_backward_weight(dY.p, dY.ld, static_cast<uint8_t*>(dYS.p), dYS.ld, fmt_dy, X.p, X.ld, static_cast<uint8_t*>(XS.p), XS.ld, fmt_x,
+                                          dY.rows, dY.cols, X.cols, block, keep, dW.p, dW.ld, s);
+  });
+  NATIVE_END
+}
+
+// (address of the job array, number of jobs, beta1, beta2, eps, step, seed, grad_scale, step_dev, stream)
+NATIVE(masked_adam_step_batched) {
+  NATIVE_ARGS(masked_adam_step_batched, 10);
+  const bsp_adam_job* jobs = static_cast<const bsp_adam_job*>(A.address(0));
+  const int n = A.i32(1), step = A.i32(5);
+  const float b1 = A.f32(2), b2 = A.f32(3), eps = A.f32(4);
+  const uint32_t seed = static_cast<uint32_t>(A.integer(6));
+  const float* scale = A.ptr<float>(7);
+  const int* step_dev = A.ptr<int>(8);
+  if (scale != nullptr) A.want_values(7, 1, 4);
+  if (step_dev != nullptr) A.want_values(8, 1, 4);
+  void* s = A.stream(9);
+  return status_of([&] { return bsp_masked_adam_step_batched(jobs, n, b1, b2, eps, step, seed, scale, step_dev, s); });
+  NATIVE_END
+}
+
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     ENTRY(group_norms), ENTRY(penalty_grad), ENTRY(prune_pack), ENTRY(percentile_threshold), ENTRY(apply_mask),
     ENTRY(prepare_batched), ENTRY(percentile_threshold_batched), ENTRY(linear_plan), ENTRY(linear_backward_weight),
     ENTRY(linear_planned), ENTRY(linear_packed), ENTRY(masked_adam_step), ENTRY(repack_values), ENTRY(transpose),
-    ENTRY(linear_gathered), ENTRY(linear_run), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(linear_gathered), ENTRY(linear_run), ENTRY(fp8_quantize), ENTRY(fp8_quantize_weight), ENTRY(linear_fp8),
+    ENTRY(linear_fp8_quantized), ENTRY(linear_fp8_backward_input), ENTRY(linear_fp8_backward_weight),
+    ENTRY(masked_adam_step_batched), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_bsp_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
