@@ -54,8 +54,6 @@ __device__ __forceinline__ void from_fp8x2(uint32_t two, float& lo, float& hi) {
   else asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
   asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
 }
-// The larger of two pairs of 16-bit magnitudes.
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
 #endif
 
 }  // namespace fp8
