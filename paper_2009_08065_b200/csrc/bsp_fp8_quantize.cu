@@ -35,29 +35,6 @@ struct QuantArgs {
 // kRows: along the rows only.  kBoth: along the columns, column sums, and along the rows where asked for.  kTile: one scale for the tile.
 enum class QuantKind { kRows, kBoth, kTile };
 
-// The larger magnitudes of two pairs of bf16 values, NaN where there is one (signs are left undefined).
-__device__ __forceinline__ uint32_t abs_max2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// The larger magnitude of a pair, as 16 bits.
-__device__ __forceinline__ uint32_t abs_max_of(uint32_t a) { return max((a >> 16) & 0x7fffu, a & 0x7fffu); }
-// Scale byte and multiplier of a block whose largest magnitude has these 16 bits.  A block with an infinity or a NaN gets scale 1 and
-// the multiplier NaN, which makes every value the NaN code.
-template <int FMT>
-__device__ __forceinline__ uint32_t block_scale(uint32_t amax16, float& inv) {
-  const bool bad = amax16 >= 0x7f80u;
-  const int byte = bad ? 127 : scale_byte(amax16 << 16, top_of(FMT));
-  inv = bad ? __uint_as_float(0x7fffffffu) : scale_inverse(byte);
-  return static_cast<uint32_t>(byte);
-}
-// Four values times their multipliers as 8 bits.
-template <int FMT>
-__device__ __forceinline__ uint32_t four_to_fp8(uint32_t x0, uint32_t x1, float i0, float i1, float i2, float i3) {
-  return to_fp8x2<FMT>(__uint_as_float(x0 << 16) * i0, __uint_as_float(x0 & 0xffff0000u) * i1) |
-         (to_fp8x2<FMT>(__uint_as_float(x1 << 16) * i2, __uint_as_float(x1 & 0xffff0000u) * i3) << 16);
-}
 // Sixteen bytes, of which n exist.
 __device__ __forceinline__ void store_sixteen(uint8_t* dst, const uint32_t (&q)[4], int n, int wide) {
   if (wide == 2 && n == 16) {

@@ -123,6 +123,8 @@ extern "C" int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ld
   size_t need = 0;
   BSP_TRY(bsp_linear_fp8_ws_bytes(tokens, k_in, &need));
   if (ws_bytes < need) return BSP_ERR_WORKSPACE;
+  if (few_tokens_ok(Wq, ldw, tokens))
+    return launch_few(Wq, ldw, WS, ldws, n_out, k_in, X, tokens, ldx, bias, act, Y, ldy, static_cast<cudaStream_t>(stream));
   uint8_t* Q = static_cast<uint8_t*>(ws);
   uint8_t* S = Q + static_cast<size_t>(tokens) * row_pitch(k_in);
   BSP_TRY(bsp_fp8_quantize(X, tokens, k_in, ldx, BSP_FP8_E4M3, Q, row_pitch(k_in), S, blocks_of(k_in), nullptr, 0, nullptr, 0, nullptr, nullptr, 0,
