@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include "bsp_fp8.cuh"
+#include "bsp_tc.cuh"
 
 namespace bsp {
 using namespace fp8;
@@ -36,7 +37,9 @@ struct AdamJob {
   int block, orient;
   float lr, decay;
   uint32_t tensor;           // its number in the call's array, for the random bits
+  uint32_t block_magic;      // row / block = the upper half of row * block_magic
   uint8_t grad16, wide, keep_wide;
+  uint32_t kb_magic;         // block of 128 / blocks in a row, the same way
 };
 struct AdamTable {
   AdamJob job[kAdamMaxJobs];
@@ -48,13 +51,18 @@ struct AdamTable {
   int step;
   const int* step_dev;
   const float* grad_scale;
+  int* status;                                     // where a wait that ran out is recorded
+  int g_size;                                      // bytes of the widest gradient
 };
 
 // The random bits of a weight: multiplications by odd constants (the fractions of 2^(1/2) and 3^(1/2)) between shifts that
 // bring the upper half down.
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
+__device__ __forceinline__ uint32_t mix_open(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x6A09E667u;
-  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  return (x ^ (x >> 15)) * 0xBB67AE85u;
+}
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x = mix_open(x);
   return x ^ (x >> 16);
 }
 __device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
@@ -92,67 +100,89 @@ __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
   return d;
 }
 
-// Two magnitudes (not negative, in the format's range) to one of their two neighbours in the format: random bits are added at
-// the upper end of what is then cut off (r: 16 of them, already at their place).  Below the smallest normal value steps are as
-// wide as just above it, so that value is added first and taken off again.
+__device__ __forceinline__ float one_if_less(float a, float b) {
+  float r;
+  asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// Two magnitudes (not negative, in the format's range) to one of their two neighbours in the format: random bits are added at the
+// upper end of what is then cut off (r: 16 of them).  Below the smallest normal value steps are as wide as just above it, so that
+// value is added first and taken off again.  (The integer pipe, at half the rate of the others, is what this kernel fills:
+// hence a comparison that gives 1 or 0 as float32, and a multiply-add for the random bits.)
 template <int FMT>
-__device__ __forceinline__ Pair round_pair(float y0, float y1, uint32_t r0, uint32_t r1) {
-  constexpr uint32_t kKeep = ~((1u << (FMT == BSP_FP8_E4M3 ? 20 : 21)) - 1u);
+__device__ __forceinline__ Pair round_pair(Pair y, uint32_t r0, uint32_t r1) {
+  constexpr int kDrop = FMT == BSP_FP8_E4M3 ? 20 : 21;
+  constexpr uint32_t kKeep = ~((1u << kDrop) - 1u);
   constexpr float kLow = FMT == BSP_FP8_E4M3 ? 0x1p-6f : 0x1p-14f;
-  const float a0 = y0 < kLow ? kLow : 0.0f, a1 = y1 < kLow ? kLow : 0.0f;
-  const Pair low = pair_of(a0, a1);
-  float z0, z1;
-  split(add(pair_of(y0, y1), low), z0, z1);
-  const Pair cut = pair_of(__uint_as_float((__float_as_uint(z0) + r0) & kKeep), __uint_as_float((__float_as_uint(z1) + r1) & kKeep));
-  return fma(low, pair_of(-1.0f), cut);
+  float y0, y1, z0, z1;
+  split(y, y0, y1);
+  const Pair below = pair_of(one_if_less(y0, kLow), one_if_less(y1, kLow));
+  split(fma(below, pair_of(kLow), y), z0, z1);
+  uint32_t u0, u1;
+  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u0) : "r"(r0), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(z0)));
+  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u1) : "r"(r1), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(z1)));
+  return fma(below, pair_of(-kLow), pair_of(__uint_as_float(u0 & kKeep), __uint_as_float(u1 & kKeep)));
+}
+// Denormal values count as zero.
+__device__ __forceinline__ float square_root(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// The largest magnitude of three, NaN if there is one.
+__device__ __forceinline__ float abs_max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
 }
 
-// Eight neighbouring weights: what the kernels for both kinds of moments share.
-struct Place {
-  int c, n;                  // first column, how many of the eight exist
-  uint32_t r, b;             // row, block of 128
-  size_t iw, ig, im, is;
-  bool wide;
-};
-__device__ __forceinline__ const AdamJob& find_job(const AdamTable& T, Place& p) {
+// The job of this CTA.
+__device__ __forceinline__ int find_job(const AdamTable& T) {
   int lo = 0, hi = T.n_jobs - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (T.first[mid] <= static_cast<int>(blockIdx.x)) lo = mid;
     else hi = mid - 1;
   }
-  const AdamJob& J = T.job[lo];
-  const uint32_t kb = static_cast<uint32_t>(blocks_of(J.cols));
-  const unsigned long long group = static_cast<unsigned long long>(blockIdx.x - T.first[lo]) * kAdamGroups + (threadIdx.x >> 4);
-  p.r = group < 0xffffffffull ? static_cast<uint32_t>(group) / kb : static_cast<uint32_t>(group / kb);
-  p.b = static_cast<uint32_t>(group - static_cast<unsigned long long>(p.r) * kb);
+  return lo;
+}
+// Eight neighbouring weights: row, block of 128 in it, first column, how many of the eight exist.
+struct Place {
+  uint32_t r, b;
+  int c, n;
+  bool wide;
+};
+__device__ __forceinline__ void settle(const AdamJob& J, Place& p) {
   p.c = static_cast<int>(p.b * kBlock + 8u * (threadIdx.x & 15u));
   p.n = p.r < static_cast<uint32_t>(J.rows) ? max(0, min(8, J.cols - p.c)) : 0;
   p.wide = J.wide != 0 && p.n == 8;
-  p.iw = static_cast<size_t>(p.r) * J.ldw + p.c;
-  p.ig = static_cast<size_t>(p.r) * J.ldg + p.c;
-  p.im = static_cast<size_t>(p.r) * J.ldm + p.c;
-  p.is = static_cast<size_t>(p.r) * kb + p.b;
-  return J;
 }
+__device__ __forceinline__ Place place_of(const AdamJob& J, uint32_t kb, unsigned long long group) {
+  Place p;
+  p.r = group < 0xffffffffull ? static_cast<uint32_t>(group) / kb : static_cast<uint32_t>(group / kb);
+  p.b = static_cast<uint32_t>(group - static_cast<unsigned long long>(p.r) * kb);
+  settle(J, p);
+  return p;
+}
+__device__ __forceinline__ size_t at(const Place& p, int ld) { return static_cast<size_t>(p.r) * ld + p.c; }
 __device__ __forceinline__ void load_weights(const AdamJob& J, const Place& p, float (&w)[8], float (&g)[8]) {
   if (p.wide) {
-    load8(J.W + p.iw, w);
+    load8(J.W + at(p, J.ldw), w);
     if (J.grad16) {
-      const uint4 h = ld_global(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(J.G) + p.ig));
+      const uint4 h = ld_global(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(J.G) + at(p, J.ldg)));
       const uint32_t hw[4] = {h.x, h.y, h.z, h.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) { g[2 * i] = __uint_as_float(hw[i] << 16); g[2 * i + 1] = __uint_as_float(hw[i] & 0xffff0000u); }
     } else {
-      load8(static_cast<const float*>(J.G) + p.ig, g);
+      load8(static_cast<const float*>(J.G) + at(p, J.ldg), g);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       w[i] = g[i] = 0.0f;
       if (i < p.n) {
-        w[i] = ld_global(J.W + p.iw + i);
-        g[i] = J.grad16 ? bf16_bits_to_float(ld_global(static_cast<const uint16_t*>(J.G) + p.ig + i)) : ld_global(static_cast<const float*>(J.G) + p.ig + i);
+        w[i] = ld_global(J.W + at(p, J.ldw) + i);
+        g[i] = J.grad16 ? bf16_bits_to_float(ld_global(static_cast<const uint16_t*>(J.G) + at(p, J.ldg) + i)) : ld_global(static_cast<const float*>(J.G) + at(p, J.ldg) + i);
       }
     }
   }
@@ -176,19 +206,24 @@ __device__ __forceinline__ uint2 load_flags(const AdamJob& J, const Place& p) {
   return k;
 }
 __device__ __forceinline__ bool kept(uint2 k, int i) { return ((i < 4 ? k.x : k.y) & (0xffu << (8 * (i & 3)))) != 0u; }
-__device__ __forceinline__ void store_weights(const AdamJob& J, const Place& p, const float (&w)[8]) {
+__device__ __forceinline__ uint4 eight_bf16(const float (&w)[8]) {
   uint32_t half[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(half[i]) : "f"(w[2 * i + 1]), "f"(w[2 * i]));
-  uint16_t* wb = J.Wb != nullptr ? J.Wb + static_cast<size_t>(p.r) * J.ldb + p.c : nullptr;
+  return make_uint4(half[0], half[1], half[2], half[3]);
+}
+__device__ __forceinline__ void store_weights(const AdamJob& J, const Place& p, const float (&w)[8]) {
+  const uint4 packed = eight_bf16(w);
+  const uint32_t half[4] = {packed.x, packed.y, packed.z, packed.w};
+  uint16_t* wb = J.Wb != nullptr ? J.Wb + at(p, J.ldb) : nullptr;
   if (p.wide) {
-    store8(J.W + p.iw, w);
-    if (wb != nullptr) *reinterpret_cast<uint4*>(wb) = make_uint4(half[0], half[1], half[2], half[3]);
+    store8(J.W + at(p, J.ldw), w);
+    if (wb != nullptr) *reinterpret_cast<uint4*>(wb) = packed;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i < p.n) {
-        J.W[p.iw + i] = w[i];
+        J.W[at(p, J.ldw) + i] = w[i];
         if (wb != nullptr) wb[i] = static_cast<uint16_t>(half[i >> 1] >> (16 * (i & 1)));
       }
     }
@@ -208,13 +243,15 @@ __device__ __forceinline__ int corrections(const AdamTable& T, float& i1, float&
 // 32-bit moments: the operations of bsp_masked_adam_step, in its order.
 __global__ void __launch_bounds__(kAdamThreads)
 adam_batched_kernel(const __grid_constant__ AdamTable T) {
-  Place p;
-  const AdamJob& J = find_job(T, p);
+  const int job = find_job(T);
+  const AdamJob& J = T.job[job];
+  const Place p = place_of(J, static_cast<uint32_t>(blocks_of(J.cols)),
+                           static_cast<unsigned long long>(blockIdx.x - T.first[job]) * kAdamGroups + (threadIdx.x >> 4));
   pdl_wait();
   pdl_launch_dependents();
   float w[8], g[8], m[8], v[8];
   load_weights(J, p, w, g);
-  float *M = static_cast<float*>(J.M) + p.im, *V = static_cast<float*>(J.V) + p.im;
+  float *M = static_cast<float*>(J.M) + at(p, J.ldm), *V = static_cast<float*>(J.V) + at(p, J.ldm);
   if (p.wide) {
     load8(M, m);
     load8(V, v);
@@ -252,112 +289,360 @@ adam_batched_kernel(const __grid_constant__ AdamTable T) {
   store_weights(J, p, w);
 }
 
-// 8-bit moments.  What bounds this one is instruction issue as much as HBM (16 bytes per weight leave 90 issue slots for a
-// warp's 32 weights), hence packed float32 operations, and the hardware's approximate square root and reciprocal (each within about a place) for
-// the update of W; the moments, which the 8-bit values follow to the last bit, are rounded as defined.
-__global__ void __launch_bounds__(kAdamThreads)
-adam_batched8_kernel(const __grid_constant__ AdamTable T) {
-  Place p;
-  const AdamJob& J = find_job(T, p);
-  pdl_wait();
-  pdl_launch_dependents();
-  float w[8], g[8];
-  load_weights(J, p, w, g);
-  uint32_t byte_m = 127u, byte_v = 127u;
-  uint2 q_m = make_uint2(0u, 0u), q_v = make_uint2(0u, 0u);
-  uint8_t *M = static_cast<uint8_t*>(J.M) + p.im, *V = static_cast<uint8_t*>(J.V) + p.im;
-  if (p.n > 0) {
-    byte_m = ld_global(J.ms + p.is);
-    byte_v = ld_global(J.vs + p.is);
-  }
-  if (p.wide) {
-    q_m = ld_global(reinterpret_cast<const uint2*>(M));
-    q_v = ld_global(reinterpret_cast<const uint2*>(V));
-  } else {
+// 8-bit moments.  HBM allows 90 issue slots (45 of the integer pipe) for a warp's 32 weights, and the arithmetic needs most of them, hence
+// packed float32 operations, and the hardware's approximate square root and reciprocal (each within about a place) for the update of W
+// (the moments, which the 8-bit values follow to the last bit, are rounded as defined).
+// Eight weights as they lie in memory.
+struct Raw {
+  uint4 w[2], g[2];            // g: float32, or bf16 in the first half
+  uint2 m, v, keep;            // keep: a byte for each weight, zero where it is pruned
+  uint32_t byte_m, byte_v;
+};
+struct Stepped {
+  float w[8];
+  uint2 m, v;
+  int byte_m, byte_v;
+};
+// What is the same for all weights of a job.
+struct Rates {
+  Pair gs, b1, b2, c1, c2, decay;      // decay: -lr weight_decay
+  float rate, eps, i2;                 // rate: -lr / (1 - beta1^step)
+  uint32_t key;
+};
+// One step of eight weights; `position` is the first one's place in its tensor.  Sixteen neighbouring threads meet in it.
+template <bool kGrad16, bool kMask>
+__device__ __forceinline__ Stepped step_eight(const Raw& x, uint32_t position, const Rates& R) {
+  Stepped out;
+  const Pair scale_m = pair_of(scale_value(x.byte_m)), scale_v = pair_of(scale_value(x.byte_v));
+  const uint32_t wb[8] = {x.w[0].x, x.w[0].y, x.w[0].z, x.w[0].w, x.w[1].x, x.w[1].y, x.w[1].z, x.w[1].w};
+  const uint32_t gb[8] = {x.g[0].x, x.g[0].y, x.g[0].z, x.g[0].w, x.g[1].x, x.g[1].y, x.g[1].z, x.g[1].w};
+  Pair m[4], v[4];
+  float most_m = 0.0f, most_v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i < p.n) {
-        (i < 4 ? q_m.x : q_m.y) |= static_cast<uint32_t>(ld_global(M + i)) << (8 * (i & 3));
-        (i < 4 ? q_v.x : q_v.y) |= static_cast<uint32_t>(ld_global(V + i)) << (8 * (i & 3));
-      }
-    }
-  }
-  const uint2 keep = load_flags(J, p);
-  float i1, i2;
-  const int step = corrections(T, i1, i2);
-  const Pair gs = pair_of(T.grad_scale != nullptr ? ld_global(T.grad_scale) : 1.0f);
-  const Pair b1 = pair_of(T.beta1), b2 = pair_of(T.beta2), c1 = pair_of(1.0f - T.beta1), c2 = pair_of(1.0f - T.beta2);
-  const Pair p1 = pair_of(i1), p2 = pair_of(i2), eps = pair_of(T.eps), lr = pair_of(-J.lr), decay = pair_of(J.decay);
-  const Pair scale_m = pair_of(scale_value(byte_m)), scale_v = pair_of(scale_value(byte_v));
-  float m[8], v[8];
-  uint32_t top_m = 0u, top_v = 0u;
-#pragma unroll
-  for (int i = 0; i < 8; i += 2) {
+  for (int i = 0; i < 4; ++i) {
     float lo, hi;
-    const Pair gi = mul(pair_of(g[i], g[i + 1]), gs);
-    from_fp8x2<BSP_FP8_E4M3>((i < 4 ? q_m.x : q_m.y) >> (8 * (i & 2)), lo, hi);
-    const Pair mi = fma(b1, mul(pair_of(lo, hi), scale_m), mul(c1, gi));
-    from_fp8x2<BSP_FP8_E5M2>((i < 4 ? q_v.x : q_v.y) >> (8 * (i & 2)), lo, hi);
-    const Pair vi = fma(b2, mul(pair_of(lo, hi), scale_v), mul(mul(c2, gi), gi));
-    split(mi, m[i], m[i + 1]);
-    split(vi, v[i], v[i + 1]);
-    top_m = max(top_m, max(__float_as_uint(m[i]) & 0x7fffffffu, __float_as_uint(m[i + 1]) & 0x7fffffffu));
-    top_v = max(top_v, max(__float_as_uint(v[i]) & 0x7fffffffu, __float_as_uint(v[i + 1]) & 0x7fffffffu));
-    split(mul(vi, p2), lo, hi);
-    asm("sqrt.approx.f32 %0, %0;" : "+f"(lo));
-    asm("sqrt.approx.f32 %0, %0;" : "+f"(hi));
-    split(add(pair_of(lo, hi), eps), lo, hi);
-    const Pair wi = pair_of(w[i], w[i + 1]);
-    const Pair upd = fma(mul(mi, p1), pair_of(reciprocal(lo), reciprocal(hi)), mul(decay, wi));
-    split(fma(lr, upd, wi), lo, hi);
-    w[i] = kept(keep, i) ? lo : 0.0f;
-    w[i + 1] = kept(keep, i + 1) ? hi : 0.0f;
+    const Pair gi = mul(kGrad16 ? pair_of(__uint_as_float(gb[i] << 16), __uint_as_float(gb[i] & 0xffff0000u))
+                                : pair_of(__uint_as_float(gb[2 * i]), __uint_as_float(gb[2 * i + 1])), R.gs);
+    from_fp8x2<BSP_FP8_E4M3>((i < 2 ? x.m.x : x.m.y) >> (16 * (i & 1)), lo, hi);
+    m[i] = fma(R.b1, mul(pair_of(lo, hi), scale_m), mul(R.c1, gi));
+    split(m[i], lo, hi);
+    most_m = abs_max3(most_m, lo, hi);
+    from_fp8x2<BSP_FP8_E5M2>((i < 2 ? x.v.x : x.v.y) >> (16 * (i & 1)), lo, hi);
+    v[i] = fma(R.b2, mul(pair_of(lo, hi), scale_v), mul(mul(R.c2, gi), gi));
+    split(v[i], lo, hi);
+    most_v = abs_max3(most_v, lo, hi);
   }
-  store_weights(J, p, w);
   const uint32_t lanes = 0xffffu << (threadIdx.x & 16u);
-  top_m = __reduce_max_sync(lanes, top_m);
-  top_v = __reduce_max_sync(lanes, top_v);
-  // a block with an infinity or a NaN becomes NaN throughout (the multiplier makes every value one), under scale 1
+  const uint32_t top_m = __reduce_max_sync(lanes, __float_as_uint(most_m)), top_v = __reduce_max_sync(lanes, __float_as_uint(most_v));
+  // The square root takes denormal values for zero, so in a block that has room for that v goes through it 2^24 times larger,
+  // and eps and the rate are 2^12 times larger too.
+  const bool room = top_v < 0x5f800000u;               // 2^64
+  const float larger = room ? 0x1p12f : 1.0f;
+  const Pair p2 = pair_of(R.i2 * (larger * larger)), eps = pair_of(R.eps * larger), rate = pair_of(R.rate * larger);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    split(mul(v[i], p2), lo, hi);
+    split(add(pair_of(square_root(lo), square_root(hi)), eps), lo, hi);
+    const Pair wi = pair_of(__uint_as_float(wb[2 * i]), __uint_as_float(wb[2 * i + 1]));
+    split(fma(R.decay, wi, fma(mul(m[i], rate), pair_of(reciprocal(lo), reciprocal(hi)), wi)), lo, hi);
+    out.w[2 * i] = !kMask || kept(x.keep, 2 * i) ? lo : 0.0f;
+    out.w[2 * i + 1] = !kMask || kept(x.keep, 2 * i + 1) ? hi : 0.0f;
+  }
+  // a block with an infinity or a NaN becomes NaN throughout, under scale 1
   const bool bad_m = top_m >= 0x7f800000u, bad_v = top_v >= 0x7f800000u;
-  const int new_m = bad_m ? 127 : scale_byte(top_m, top_of(BSP_FP8_E4M3)), new_v = bad_v ? 127 : scale_byte(top_v, top_of(BSP_FP8_E5M2));
-  const Pair inv_m = pair_of(scale_inverse(new_m)), inv_v = pair_of(scale_inverse(new_v));
-  const uint32_t key = mix(T.seed + 0x9E3779B9u * static_cast<uint32_t>(step) + 0xBB67AE85u * J.tensor);
-  const uint32_t at = p.r * static_cast<uint32_t>(J.cols) + static_cast<uint32_t>(p.c) + key;
+  out.byte_m = bad_m ? 127 : scale_byte(top_m, top_of(BSP_FP8_E4M3));
+  out.byte_v = bad_v ? 127 : scale_byte(top_v, top_of(BSP_FP8_E5M2));
+  const Pair inv_m = pair_of(scale_inverse(out.byte_m)), inv_v = pair_of(scale_inverse(out.byte_v));
   uint32_t out_m[4], out_v[4];
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    const uint32_t h0 = mix(at + static_cast<uint32_t>(i)), h1 = mix(at + static_cast<uint32_t>(i + 1));
-    float lo, hi;
-    split(mul(pair_of(fabsf(m[i]), fabsf(m[i + 1])), inv_m), lo, hi);
-    split(round_pair<BSP_FP8_E4M3>(lo, hi, (h0 << 4) & 0xffff0u, (h1 << 4) & 0xffff0u), lo, hi);
-    out_m[i >> 1] = to_fp8x2<BSP_FP8_E4M3>(copysignf(lo, m[i]), copysignf(hi, m[i + 1]));
-    // (a positive value below the smallest one becomes that, which random bits leave as it is)
-    split(mul(pair_of(v[i], v[i + 1]), inv_v), lo, hi);
-    lo = v[i] > 0.0f ? fmaxf(lo, 0x1p-16f) : 0.0f;
-    hi = v[i + 1] > 0.0f ? fmaxf(hi, 0x1p-16f) : 0.0f;
-    split(round_pair<BSP_FP8_E5M2>(lo, hi, (h0 >> 11) & 0x1fffe0u, (h1 >> 11) & 0x1fffe0u), lo, hi);
-    out_v[i >> 1] = to_fp8x2<BSP_FP8_E5M2>(lo, hi);
-  }
-  q_m = make_uint2(out_m[0] | (out_m[1] << 16), out_m[2] | (out_m[3] << 16));
-  q_v = make_uint2(out_v[0] | (out_v[1] << 16), out_v[2] | (out_v[3] << 16));
-  if (bad_m) q_m = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
-  if (bad_v) q_v = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
-  if ((threadIdx.x & 15u) == 0 && p.n > 0) {
-    J.ms[p.is] = static_cast<uint8_t>(new_m);
-    J.vs[p.is] = static_cast<uint8_t>(new_v);
-  }
-  if (p.wide) {
-    *reinterpret_cast<uint2*>(M) = q_m;
-    *reinterpret_cast<uint2*>(V) = q_v;
-  } else {
+  for (int i = 0; i < 4; ++i) {
+    uint32_t m_bits[2], v_bits[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i < p.n) {
-        M[i] = static_cast<uint8_t>((i < 4 ? q_m.x : q_m.y) >> (8 * (i & 3)));
-        V[i] = static_cast<uint8_t>((i < 4 ? q_v.x : q_v.y) >> (8 * (i & 3)));
-      }
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t h = mix_open(position + static_cast<uint32_t>(2 * i + e) + R.key);
+      v_bits[e] = h >> 16;                             // the upper and the lower half of h ^ (h >> 16)
+      m_bits[e] = (h ^ v_bits[e]) & 0xffffu;
+    }
+    float lo, hi, a, b;
+    split(m[i], a, b);
+    split(round_pair<BSP_FP8_E4M3>(mul(pair_of(fabsf(a), fabsf(b)), inv_m), m_bits[0], m_bits[1]), lo, hi);
+    out_m[i] = to_fp8x2<BSP_FP8_E4M3>(copysignf(lo, a), copysignf(hi, b));
+    // A positive value below the smallest one becomes that, which random bits leave as it is.
+    split(v[i], lo, hi);
+    split(mul(pair_of(one_if_less(0.0f, lo), one_if_less(0.0f, hi)), pair_of(0x1p-16f)), a, b);
+    split(mul(v[i], inv_v), lo, hi);
+    split(round_pair<BSP_FP8_E5M2>(pair_of(fmaxf(lo, a), fmaxf(hi, b)), v_bits[0], v_bits[1]), lo, hi);
+    out_v[i] = to_fp8x2<BSP_FP8_E5M2>(lo, hi);
+  }
+  out.m = make_uint2(out_m[0] | (out_m[1] << 16), out_m[2] | (out_m[3] << 16));
+  out.v = make_uint2(out_v[0] | (out_v[1] << 16), out_v[2] | (out_v[3] << 16));
+  if (bad_m) out.m = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
+  if (bad_v) out.v = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
+  return out;
+}
+
+__device__ __forceinline__ void rates(const AdamTable& T, const AdamJob& J, Rates& R) {
+  float i1;
+  const int step = corrections(T, i1, R.i2);
+  R.key = mix(T.seed + 0x9E3779B9u * static_cast<uint32_t>(step) + 0xBB67AE85u * J.tensor);
+  R.gs = pair_of(T.grad_scale != nullptr ? ld_global(T.grad_scale) : 1.0f);
+  R.b1 = pair_of(T.beta1); R.b2 = pair_of(T.beta2); R.c1 = pair_of(1.0f - T.beta1); R.c2 = pair_of(1.0f - T.beta2);
+  R.rate = -J.lr * i1; R.eps = T.eps; R.decay = pair_of(-J.lr * J.decay);
+}
+
+// Tensors without gaps whose rows are whole pieces of eight, masked along columns or not at all.  Sixteen blocks of 128 lie next to each
+// other in memory then, and reach shared memory by bulk copies, two such chunks ahead: 100 KB on their way per SM.  (A fourth stage takes its room from L1, where the flags of a block's
+// rows are found again: 302 M weights 1006 us with three stages, 1054 with four.)  Loads to registers,
+// also one turn ahead, came to half of that at 24 warps per SM, and the kernel waited for them: 302 M weights 1088 us and more however little was
+// computed.  CTAs that run at once work on neighbouring chunks.
+constexpr int kChunk = kAdamGroups * kBlock;       // weights
+constexpr int kStreamCtas = 3;                     // of an SM
+constexpr int kStreamStages = 3;
+constexpr int kStreamW = kChunk * 4, kStreamQ = kChunk + 32, kStreamS = 32;      // bytes (8-bit values begin anywhere: copied from a multiple of 16 on)
+constexpr int kStreamHead = 16 * kStreamStages + 80;               // mbarriers, a flag
+// A stage: W, m, v, the scales of both, and the gradients of the widest type among the launch's tensors.
+__host__ __device__ constexpr int stream_stage(int g_size) { return kStreamW + 2 * kStreamQ + 2 * kStreamS + kChunk * g_size; }
+static_assert(kStreamHead % 16 == 0 && stream_stage(2) % 16 == 0, "alignment of bulk copies");
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// The bytes [p, p + n) in whole pieces of 16; they begin (p % 16) bytes behind dst.
+__device__ __forceinline__ uint32_t pieces16(const uint8_t* p, uint32_t n) { return (n + static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) & 15u) + 15u) & ~15u; }
+__device__ __forceinline__ const uint8_t* floor16(const uint8_t* p) { return p - (reinterpret_cast<uintptr_t>(p) & 15u); }
+// First weight of a block of 128 in its tensor, and its row.
+__device__ __forceinline__ size_t block_begin(const AdamJob& J, uint32_t kb, uint32_t group, uint32_t& r, uint32_t& c) {
+  r = J.kb_magic != 0u ? __umulhi(group, J.kb_magic) : group;
+  c = (group - r * kb) * kBlock;
+  return static_cast<size_t>(r) * static_cast<uint32_t>(J.cols) + c;
+}
+// Asks for a chunk of a job, by a whole warp: lanes 0 to 5 one copy each.
+constexpr int kCopies = 6;
+__device__ __forceinline__ void ask_for(const AdamJob& J, uint32_t chunk, uint32_t stage, uint32_t bar) {
+  const uint32_t kb = static_cast<uint32_t>(blocks_of(J.cols)), groups = static_cast<uint32_t>(J.rows) * kb;
+  const uint32_t first = chunk * kAdamGroups, behind = min(first + kAdamGroups, groups);
+  uint32_t r, c;
+  const size_t e = block_begin(J, kb, first, r, c);
+  const size_t end = behind == groups ? static_cast<size_t>(J.rows) * static_cast<uint32_t>(J.cols) : block_begin(J, kb, behind, r, c);
+  const uint32_t lane = threadIdx.x & 31u;
+  const bool scales = lane == 3u || lane == 4u;
+  const uint32_t size = lane == 0u ? 4u : lane == 5u ? (J.grad16 ? 2u : 4u) : 1u;
+  const void* from = lane == 0u ? J.W : lane == 1u ? J.M : lane == 2u ? J.V : lane == 3u ? J.ms : lane == 4u ? J.vs : J.G;
+  const uint32_t to = lane == 0u ? 0u : lane == 1u ? kStreamW : lane == 2u ? kStreamW + kStreamQ : lane == 3u ? kStreamW + 2 * kStreamQ
+                      : lane == 4u ? kStreamW + 2 * kStreamQ + kStreamS : kStreamW + 2 * kStreamQ + 2 * kStreamS;
+  const uint8_t* src = static_cast<const uint8_t*>(from) + (scales ? static_cast<size_t>(first) : e * size);
+  const uint32_t bytes = pieces16(src, scales ? behind - first : static_cast<uint32_t>(end - e) * size);
+  if (lane < kCopies) {
+    tc::mbar_arrive_expect_tx(bar, bytes);
+    bulk_load(stage + to, floor16(src), bytes, bar);
+  }
+  __syncwarp();
+}
+
+// A thread's eight weights of a chunk: block of 128, row and column of the first, and their flags, asked for a turn ahead.
+struct Turn {
+  uint32_t group, r, c;
+  uint2 keep;
+};
+// kRagged: rows end inside a block of 128.  (Where they don't, a block's sixteen threads all have weights or none have, and those that have none
+// may work on what shared memory holds.)
+template <bool kGrad16, bool kMask, bool kRagged>
+__device__ __forceinline__ void chunk_step(const AdamJob& J, const Turn& t, uint32_t chunk, uint32_t stage, const Rates& R) {
+  const size_t e = static_cast<size_t>(t.r) * static_cast<uint32_t>(J.cols) + t.c;
+  const bool exists = t.r < static_cast<uint32_t>(J.rows) && (!kRagged || t.c < static_cast<uint32_t>(J.cols));
+  uint32_t i = 8u * threadIdx.x;                     // place in the chunk
+  size_t e0;
+  if (kRagged) {
+    uint32_t r, c;
+    e0 = block_begin(J, static_cast<uint32_t>(blocks_of(J.cols)), chunk * kAdamGroups, r, c);
+    i = exists ? static_cast<uint32_t>(e - e0) : 0u;
+  } else {
+    e0 = e - i;
+  }
+  uint8_t *M = static_cast<uint8_t*>(J.M), *V = static_cast<uint8_t*>(J.V);
+  auto two = [](uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    return v;
+  };
+  Raw x;
+  x.w[0] = tc::ld_shared_v4(stage + 4u * i);
+  x.w[1] = tc::ld_shared_v4(stage + 4u * i + 16u);
+  stage += kStreamW;
+  x.m = two(stage + i + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(M) + e0) & 15u));
+  x.v = two(stage + kStreamQ + i + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(V) + e0) & 15u));
+  stage += 2 * kStreamQ;
+  auto byte = [](uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+  };
+  const uint32_t block = threadIdx.x >> 4;             // of the chunk
+  x.byte_m = byte(stage + block + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(J.ms) + t.group - block) & 15u));
+  x.byte_v = byte(stage + kStreamS + block + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(J.vs) + t.group - block) & 15u));
+  stage += 2 * kStreamS;
+  x.g[0] = tc::ld_shared_v4(stage + (kGrad16 ? 2u : 4u) * i);
+  if (!kGrad16) x.g[1] = tc::ld_shared_v4(stage + 4u * i + 16u);
+  if (kRagged && !exists) {
+    x.g[0] = x.g[1] = make_uint4(0u, 0u, 0u, 0u);
+    x.m = x.v = make_uint2(0u, 0u);
+  }
+  x.keep = t.keep;
+  const Stepped z = step_eight<kGrad16, kMask>(x, static_cast<uint32_t>(e), R);
+  if (exists) {
+    store8(J.W + e, z.w);
+    *reinterpret_cast<uint2*>(M + e) = z.m;
+    *reinterpret_cast<uint2*>(V + e) = z.v;
+    if (J.Wb != nullptr) *reinterpret_cast<uint4*>(J.Wb + e) = eight_bf16(z.w);
+    if ((threadIdx.x & 15u) == 0u) {
+      J.ms[t.group] = static_cast<uint8_t>(z.byte_m);
+      J.vs[t.group] = static_cast<uint8_t>(z.byte_v);
     }
   }
+}
+template <bool kRagged>
+__device__ __forceinline__ void chunk_step(const AdamJob& J, const Turn& t, uint32_t chunk, uint32_t stage, const Rates& R) {
+  if (J.grad16) {
+    if (J.keep != nullptr) chunk_step<true, true, kRagged>(J, t, chunk, stage, R);
+    else chunk_step<true, false, kRagged>(J, t, chunk, stage, R);
+  } else {
+    if (J.keep != nullptr) chunk_step<false, true, kRagged>(J, t, chunk, stage, R);
+    else chunk_step<false, false, kRagged>(J, t, chunk, stage, R);
+  }
+}
+
+__global__ void __launch_bounds__(kAdamThreads, kStreamCtas)
+adam_stream8_kernel(const __grid_constant__ AdamTable T) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  const uint32_t full = tc::smem_u32(smem), empty = full + 8u * kStreamStages, base = full + kStreamHead;
+  volatile uint32_t* timed_out = reinterpret_cast<volatile uint32_t*>(smem + 16 * kStreamStages);
+  constexpr int stages = kStreamStages;
+  const int stage_bytes = stream_stage(T.g_size);
+  if (threadIdx.x == 0) {
+    *timed_out = 0u;
+    for (int s = 0; s < stages; ++s) {
+      tc::mbar_init(full + 8u * s, kCopies);
+      tc::mbar_init(empty + 8u * s, kAdamThreads / 32);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tc::fence_async_smem();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
+  const int chunks = T.first[T.n_jobs];
+  int asked_job = 0;
+  auto ask = [&](int chunk, int stage) {
+    while (chunk >= T.first[asked_job + 1]) ++asked_job;
+    ask_for(T.job[asked_job], static_cast<uint32_t>(chunk - T.first[asked_job]), base + stage * stage_bytes, full + 8u * stage);
+  };
+  const int grid = static_cast<int>(gridDim.x);
+  if (threadIdx.x < 32) {
+    for (int s = 0; s < stages && static_cast<int>(blockIdx.x) + s * grid < chunks; ++s) ask(blockIdx.x + s * grid, s);
+  }
+  int job = -1, stage = 0;
+  uint32_t turn = 0u;
+  uint32_t phase = 0u, last = 0u;                    // last: parity of the stage before
+  Rates R;
+  bool ok = true;
+  int next_job = 0;
+  Turn next;
+  auto look_up = [&](int chunk) {
+    while (chunk >= T.first[next_job + 1]) ++next_job;
+    const AdamJob& J = T.job[next_job];
+    next.group = static_cast<uint32_t>(chunk - T.first[next_job]) * kAdamGroups + (threadIdx.x >> 4);
+    block_begin(J, static_cast<uint32_t>(blocks_of(J.cols)), next.group, next.r, next.c);
+    next.c += 8u * (threadIdx.x & 15u);
+    if (J.keep != nullptr && next.r < static_cast<uint32_t>(J.rows) && next.c < static_cast<uint32_t>(J.cols))
+      next.keep = ld_global(reinterpret_cast<const uint2*>(J.keep + static_cast<size_t>(J.block_magic != 0u ? __umulhi(next.r, J.block_magic) : next.r) * J.cols + next.c));
+  };
+  next.keep = make_uint2(0u, 0u);
+  look_up(blockIdx.x);
+  for (int chunk = blockIdx.x; chunk < chunks; chunk += grid) {
+    const Turn now = next;
+    if (next_job != job) {
+      job = next_job;
+      rates(T, T.job[job], R);
+    }
+    const AdamJob& J = T.job[job];
+    if (!tc::mbar_wait(full + 8u * stage, phase, T.status)) { ok = false; break; }
+    if (chunk + grid < chunks) look_up(chunk + grid);
+    const uint32_t at_stage = base + stage * stage_bytes, number = static_cast<uint32_t>(chunk - T.first[job]);
+    if (J.cols % kBlock != 0) chunk_step<true>(J, now, number, at_stage, R);
+    else chunk_step<false>(J, now, number, at_stage, R);
+    __syncwarp();
+    if ((threadIdx.x & 31u) == 0) tc::mbar_arrive(empty + 8u * stage);
+    // The stage of the turn before, which the slowest warp has left by now or soon will have, is filled again, by each warp in turn: the warp
+    // that asks falls behind the others.
+    const int refill = chunk + (stages - 1) * grid;
+    if (threadIdx.x >> 5 == (turn & 7u) && turn > 0 && refill < chunks) {
+      const int before = stage == 0 ? stages - 1 : stage - 1;
+      if (!tc::mbar_wait_warp(empty + 8u * before, last, T.status)) { ok = false; break; }
+      ask(refill, before);
+    }
+    ++turn;
+    last = phase;
+    if (++stage == stages) { stage = 0; phase ^= 1u; }
+  }
+  if (!ok) tc::record_timeout(T.status, timed_out);
+  __syncthreads();
+  tc::quiet_period(timed_out);                       // (copies in flight still land in this CTA's shared memory)
+}
+
+// Any other tensor.
+__global__ void __launch_bounds__(kAdamThreads)
+adam_batched8_kernel(const __grid_constant__ AdamTable T) {
+  const int job = find_job(T);
+  const AdamJob& J = T.job[job];
+  const uint32_t kb = static_cast<uint32_t>(blocks_of(J.cols));
+  const Place p = place_of(J, kb, static_cast<unsigned long long>(blockIdx.x - T.first[job]) * kAdamGroups + (threadIdx.x >> 4));
+  uint8_t *M = static_cast<uint8_t*>(J.M) + at(p, J.ldm), *V = static_cast<uint8_t*>(J.V) + at(p, J.ldm);
+  const size_t is = static_cast<size_t>(p.r) * kb + p.b;
+  pdl_wait();
+  pdl_launch_dependents();
+  Rates R;
+  rates(T, J, R);
+  float w[8], g[8];
+  load_weights(J, p, w, g);
+  uint32_t q[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i < p.n) {
+      q[i >> 2] |= static_cast<uint32_t>(ld_global(M + i)) << (8 * (i & 3));
+      q[2 + (i >> 2)] |= static_cast<uint32_t>(ld_global(V + i)) << (8 * (i & 3));
+    }
+  }
+  auto four = [](const float* f) { return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])); };
+  Raw x;
+  x.w[0] = four(w); x.w[1] = four(w + 4); x.g[0] = four(g); x.g[1] = four(g + 4);
+  x.m = make_uint2(q[0], q[1]);
+  x.v = make_uint2(q[2], q[3]);
+  x.keep = load_flags(J, p);
+  x.byte_m = p.n > 0 ? ld_global(J.ms + is) : 127u;
+  x.byte_v = p.n > 0 ? ld_global(J.vs + is) : 127u;
+  const Stepped z = step_eight<false, true>(x, p.r * static_cast<uint32_t>(J.cols) + static_cast<uint32_t>(p.c), R);
+  store_weights(J, p, z.w);
+  if ((threadIdx.x & 15u) == 0 && p.n > 0) {
+    J.ms[is] = static_cast<uint8_t>(z.byte_m);
+    J.vs[is] = static_cast<uint8_t>(z.byte_v);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i < p.n) {
+      M[i] = static_cast<uint8_t>((i < 4 ? z.m.x : z.m.y) >> (8 * (i & 3)));
+      V[i] = static_cast<uint8_t>((i < 4 ? z.v.x : z.v.y) >> (8 * (i & 3)));
+    }
+  }
+}
+
+// Whether a tensor of 8-bit moments goes through adam_stream8_kernel (its numbers of blocks and rows have to divide by multiplication).
+bool streams(const bsp_adam_job& a, const AdamJob& j) {
+  const unsigned long long kb = blocks_of(a.cols), most = 1ull << 32;
+  return a.state_bits == 8 && j.wide && a.cols % 8 == 0 && a.ldw == a.cols && a.ldg == a.cols && a.ldm == a.cols && (a.W_bf16 == nullptr || a.ldb == a.cols) &&
+         (static_cast<unsigned long long>(a.rows) * kb + kAdamGroups) * kb < most &&
+         (a.keep == nullptr || (a.orient == BSP_ORIENT_C && j.keep_wide && (static_cast<unsigned long long>(a.rows) + kAdamGroups) * a.block < most));
 }
 
 // Checks one job and fills its entry; *ctas receives what it needs.
@@ -388,6 +673,10 @@ int make_job(const bsp_adam_job& a, uint32_t tensor, AdamJob* j, long long* ctas
   j->wide = aligned_to(a.W, 16) && a.ldw % 4 == 0 && aligned_to(a.grad, 16) && a.ldg % (grad16 ? 8 : 4) == 0 && aligned_to(a.m, bits8 ? 8 : 16) &&
             aligned_to(a.v, bits8 ? 8 : 16) && a.ldm % (bits8 ? 8 : 4) == 0 && (a.W_bf16 == nullptr || (aligned_to(a.W_bf16, 16) && a.ldb % 8 == 0));
   j->keep_wide = aligned_to(a.keep, 8) && a.cols % 8 == 0;
+  // ceil(2^32 / d): exact for numbers below 2^32 / d; 0 for d = 1
+  auto magic = [](long long d) { return d > 1 ? static_cast<uint32_t>((0x100000000ll + d - 1) / d) : 0u; };
+  j->block_magic = magic(j->block);
+  j->kb_magic = magic(blocks_of(a.cols));
   const long long groups = static_cast<long long>(a.rows) * blocks_of(a.cols);
   *ctas = (groups + kAdamGroups - 1) / kAdamGroups;
   return *ctas > 0x3fffffffLL ? BSP_ERR_UNSUPPORTED : BSP_OK;
@@ -408,6 +697,9 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
     long long ctas;
     BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &T.job[0], &ctas));
   }
+  TcDevice* dev = tc_device();
+  if (dev == nullptr) return BSP_ERR_CUDA;
+  T.status = dev->status;
   T.beta1 = beta1; T.beta2 = beta2; T.eps = eps;
   T.inv_c1 = T.inv_c2 = 0.0f;
   if (step_dev == nullptr) {                          // bias corrections in double on the host, rounded once
@@ -418,23 +710,35 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
   T.log_beta2 = static_cast<float>(log(static_cast<double>(beta2)));
   T.seed = seed; T.step = step; T.step_dev = step_dev; T.grad_scale = grad_scale;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // one kernel for each kind of moments, and launches of up to kAdamMaxJobs tensors of that kind
-  for (const int bits : {8, 32}) {
-    if (bits == 8 && T.eps > 0.0f && T.eps < FLT_MIN) T.eps = FLT_MIN;     // (a denormal one has no reciprocal there)
+  // one kernel for each kind of tensor, and launches of up to kAdamMaxJobs tensors of that kind
+  enum { kStream8, kAny8, kBits32 };
+  for (const int kind : {kStream8, kAny8, kBits32}) {
+    if (kind != kBits32 && T.eps > 0.0f && T.eps < FLT_MIN) T.eps = FLT_MIN;     // (a denormal one has no reciprocal there)
     for (int i = 0; i < n_jobs;) {
       long long total = 0;
       T.n_jobs = 0;
+      T.g_size = 2;
       for (; i < n_jobs && T.n_jobs < kAdamMaxJobs; ++i) {
-        if (jobs[i].state_bits != bits) continue;
+        AdamJob& j = T.job[T.n_jobs];
         long long ctas;
-        BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &T.job[T.n_jobs], &ctas));
-        if (T.n_jobs > 0 && total + ctas > 0x7fffffffLL) break;
+        BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &j, &ctas));
+        if (kind != (jobs[i].state_bits == 32 ? kBits32 : streams(jobs[i], j) ? kStream8 : kAny8)) continue;
+        if (T.n_jobs > 0 && total + ctas > 0x3fffffffLL) break;
+        if (!j.grad16) T.g_size = 4;
         T.first[T.n_jobs++] = static_cast<int>(total);
         total += ctas;
       }
       if (T.n_jobs == 0) break;
       T.first[T.n_jobs] = static_cast<int>(total);
-      BSP_CUDA_TRY(launch_pdl(bits == 8 ? adam_batched8_kernel : adam_batched_kernel, dim3(static_cast<unsigned>(total)), dim3(kAdamThreads), 0, s, T));
+      if (kind == kStream8) {
+        static OncePerDevice once;
+        const int smem = kStreamHead + kStreamStages * stream_stage(T.g_size);
+        BSP_TRY(allow_dynamic_smem(once, adam_stream8_kernel, kStreamHead + kStreamStages * stream_stage(4)));
+        const long long grid = total < static_cast<long long>(kStreamCtas) * dev->sms ? total : static_cast<long long>(kStreamCtas) * dev->sms;
+        BSP_CUDA_TRY(launch_pdl(adam_stream8_kernel, dim3(static_cast<unsigned>(grid)), dim3(kAdamThreads), smem, s, T));
+      } else {
+        BSP_CUDA_TRY(launch_pdl(kind == kAny8 ? adam_batched8_kernel : adam_batched_kernel, dim3(static_cast<unsigned>(total)), dim3(kAdamThreads), 0, s, T));
+      }
     }
     T.eps = eps;
   }

@@ -121,6 +121,33 @@ def test_three_steps(bits, grad16):
     run(make(bits, grad16), (1, 2, 3), 12345)
 
 
+# tensors without gaps: a part of a chunk, several rows in one, rows that end inside a block of 128, more chunks than run at once
+STREAM = [(1, 8, 0, 0, 0), (3, 128, 0, 1, 0), (100, 8, 0, 4, 0), (16, 200, 0, 2, 0), (48, 920, 0, 12, 0), (7, 4096, 0, 0, 0), (1536, 1024, 0, 16, 0), (5, 136, 0, 5, 0)]
+
+
+@pytest.mark.parametrize("grad16", [False, True])
+def test_three_steps_without_gaps(grad16):
+    run(make(8, grad16, STREAM), (1, 2, 3), 99, clip=0.5)
+
+
+def test_views_that_begin_inside_an_arena():
+    """8-bit moments that begin at multiples of 8 but not of 16 bytes, tensors right behind one another."""
+    tensors = make(8, True, [(1, 8, 0, 0, 0), (3, 136, 0, 3, 0), (1, 24, 0, 0, 0), (40, 200, 0, 4, 0), (1, 920, 0, 0, 0)])
+    total = sum(t.rows * t.cols for t in tensors)
+    at = 0
+    for name in ("W", "M", "V", "Wb", "G"):
+        arena = torch.zeros(total, dtype=getattr(tensors[0], name).dtype, device=DEV)
+        at = 0
+        for t in tensors:
+            view = arena[at:at + t.rows * t.cols].view(t.rows, t.cols)
+            view.copy_(getattr(t, name))
+            setattr(t, name, view)
+            at += t.rows * t.cols
+    for t in tensors:
+        t.job.W, t.job.m, t.job.v, t.job.W_bf16, t.job.grad = t.W, t.M, t.V, t.Wb, t.G
+    run(tensors, (1, 2), 4)
+
+
 def test_clipped_and_late():
     run(make(8, True), (1, 1000, 2 ** 31 - 1), 2 ** 32 - 1, clip=0.37)
 
