@@ -19,27 +19,38 @@ namespace {
 
 constexpr int kFewRows = 16;                 // outputs per CTA
 constexpr int kFewMaxWarps = 16;
+// Clusters of 2 or 4 CTAs share the contraction of 16 outputs while they are at most this many CTAs and each has this many blocks of 128.
+constexpr int kFewCtas = 296, kFewLeastBlocks = 8;
 
 struct FewArgs {
   const uint8_t* W;
   int ldw;
   const uint8_t* S;
   int lds, n_out, k_in;
-  const uint16_t* X;
-  int tokens, ldx, wide;     // 16-byte loads of X
+  const void* X;             // bf16, or 8 bits with the scales XS
+  int tokens, ldx, wide;     // 16-byte loads of bf16 X
+  const uint8_t* XS;
+  int ldxs;
   const uint16_t* bias;
   int act;
   uint16_t* Y;
   int ldy;
 };
 
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// e4m3 weights times activations of either format.
+template <int FMT>
+__device__ __forceinline__ void mma_fp8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (FMT == BSP_FP8_E4M3)
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e5m2.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Sixteen 8-bit weights from column k on, zeros where the row has ended.
-__device__ __forceinline__ uint4 weight_piece(const uint8_t* row, int k, int k_in, bool exists) {
+// Sixteen 8-bit values from column k on, zeros where the row has ended.
+__device__ __forceinline__ uint4 byte_piece(const uint8_t* row, int k, int k_in, bool exists) {
   if (!exists || k >= k_in) return make_uint4(0u, 0u, 0u, 0u);
   if (k + 16 <= k_in) return ld_global(reinterpret_cast<const uint4*>(row + k));
   uint32_t w[4] = {0u, 0u, 0u, 0u};
@@ -59,56 +70,84 @@ __device__ __forceinline__ uint4 token_piece(const uint16_t* row, int k, int k_i
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// GROUPS: groups of eight tokens.
-template <int GROUPS>
+// GROUPS: groups of eight tokens.  kReady: the activations are in 8 bits (of format FMT) already.
+template <int GROUPS, bool kReady, int FMT>
 __global__ void __launch_bounds__(32 * kFewMaxWarps)
 linear_few_kernel(FewArgs A) {
   extern __shared__ float s_part[];          // [warp][token][16 outputs]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * kFewRows;
+  const int n0 = static_cast<int>(blockIdx.x / tc::cluster_size()) * kFewRows;
   const int blocks = blocks_of(A.k_in);
   float acc[GROUPS][4] = {};
   pdl_wait();
   pdl_launch_dependents();
-  for (int kb = warp; kb < blocks; kb += warps) {
-    const int k = kb * kBlock + 16 * t;
+  // Everything a block needs is asked for before any of it is used.
+  struct Block {
     uint4 w[2][2];                           // [half of the block][row g, row g + 8]
+    uint4 x[GROUPS][2][kReady ? 1 : 2];
+    uint32_t scale, scale_x[kReady ? GROUPS : 1];
+  };
+  auto load = [&](int kb) {
+    Block q;
+    const int k = kb * kBlock + 16 * t;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int n = n0 + g + 8 * u;
-        w[h][u] = weight_piece(A.W + static_cast<size_t>(n) * A.ldw, k + 64 * h, A.k_in, n < A.n_out);
+        q.w[h][u] = byte_piece(A.W + static_cast<size_t>(n) * A.ldw, k + 64 * h, A.k_in, n < A.n_out);
       }
-    const float scale_w = scale_value(ld_global(A.S + static_cast<size_t>(n0 / kBlock) * A.lds + kb));
+    q.scale = ld_global(A.S + static_cast<size_t>(n0 / kBlock) * A.lds + kb);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
       const int token = 8 * j + g;
-      const uint16_t* row = A.X + static_cast<size_t>(token) * A.ldx;
-      uint4 x[2][2];
+      const bool exists = token < A.tokens;
+      if constexpr (kReady) {
+        const uint8_t* row = static_cast<const uint8_t*>(A.X) + static_cast<size_t>(token) * A.ldx;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) q.x[j][h][0] = byte_piece(row, k + 64 * h, A.k_in, exists);
+        q.scale_x[j] = exists ? ld_global(A.XS + static_cast<size_t>(token) * A.ldxs + kb) : 127u;
+      } else {
+        const uint16_t* row = static_cast<const uint16_t*>(A.X) + static_cast<size_t>(token) * A.ldx;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) x[h][u] = token_piece(row, k + 64 * h + 8 * u, A.k_in, token < A.tokens, A.wide);
-      uint32_t m = 0u;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+          for (int u = 0; u < 2; ++u) q.x[j][h][u] = token_piece(row, k + 64 * h + 8 * u, A.k_in, exists, A.wide);
+      }
+    }
+    return q;
+  };
+  auto multiply = [&](const Block& q) {
+    const float scale_w = scale_value(q.scale);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) m = abs_max2(m, abs_max2(abs_max2(x[h][u].x, x[h][u].y), abs_max2(x[h][u].z, x[h][u].w)));
-      m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      float inv;
-      const float scale_x = scale_value(block_scale<BSP_FP8_E4M3>(abs_max_of(m), inv));
-      float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < GROUPS; ++j) {
+      float c[4] = {0.0f, 0.0f, 0.0f, 0.0f}, scale_x;
+      uint4 v[2];                            // the token's values in 8 bits
+      if constexpr (kReady) {
+        scale_x = scale_value(q.scale_x[j]);
+        v[0] = q.x[j][0][0];
+        v[1] = q.x[j][1][0];
+      } else {
+        const uint4 (&x)[2][2] = q.x[j];
+        uint32_t m = 0u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) m = abs_max2(m, abs_max2(abs_max2(x[h][u].x, x[h][u].y), abs_max2(x[h][u].z, x[h][u].w)));
+        m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        float inv;
+        scale_x = scale_value(block_scale<FMT>(abs_max_of(m), inv));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          v[h] = make_uint4(four_to_fp8<FMT>(x[h][0].x, x[h][0].y, inv, inv, inv, inv), four_to_fp8<FMT>(x[h][0].z, x[h][0].w, inv, inv, inv, inv),
+                            four_to_fp8<FMT>(x[h][1].x, x[h][1].y, inv, inv, inv, inv), four_to_fp8<FMT>(x[h][1].z, x[h][1].w, inv, inv, inv, inv));
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t q0 = four_to_fp8<BSP_FP8_E4M3>(x[h][0].x, x[h][0].y, inv, inv, inv, inv);
-        const uint32_t q1 = four_to_fp8<BSP_FP8_E4M3>(x[h][0].z, x[h][0].w, inv, inv, inv, inv);
-        const uint32_t q2 = four_to_fp8<BSP_FP8_E4M3>(x[h][1].x, x[h][1].y, inv, inv, inv, inv);
-        const uint32_t q3 = four_to_fp8<BSP_FP8_E4M3>(x[h][1].z, x[h][1].w, inv, inv, inv, inv);
-        mma_e4m3(c, w[h][0].x, w[h][1].x, w[h][0].y, w[h][1].y, q0, q1);
-        mma_e4m3(c, w[h][0].z, w[h][1].z, w[h][0].w, w[h][1].w, q2, q3);
+        mma_fp8<FMT>(c, q.w[h][0].x, q.w[h][1].x, q.w[h][0].y, q.w[h][1].y, v[h].x, v[h].y);
+        mma_fp8<FMT>(c, q.w[h][0].z, q.w[h][1].z, q.w[h][0].w, q.w[h][1].w, v[h].z, v[h].w);
       }
       // this lane's outputs are of tokens 2 t and 2 t + 1 of the group
       const float s0 = scale_w * __shfl_sync(0xffffffffu, scale_x, 8 * t), s1 = scale_w * __shfl_sync(0xffffffffu, scale_x, 8 * t + 4);
@@ -117,17 +156,42 @@ linear_few_kernel(FewArgs A) {
       acc[j][2] = __fmaf_rn(c[2], s0, acc[j][2]);
       acc[j][3] = __fmaf_rn(c[3], s1, acc[j][3]);
     }
+  };
+  // the contraction's blocks are dealt to the warps of all CTAs of the cluster
+  const int ranks = static_cast<int>(tc::cluster_size()), rank = static_cast<int>(tc::cluster_rank()), all = warps * ranks;
+  for (int kb = warp * ranks + rank; kb < blocks; kb += all) {
+    const Block p = load(kb);
+    __syncwarp();                            // (the assembler would move loads down to save registers)
+    multiply(p);
   }
 #pragma unroll
   for (int j = 0; j < GROUPS; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) s_part[(warp * 8 * GROUPS + 8 * j + 2 * t + (e & 1)) * kFewRows + g + 8 * (e >> 1)] = acc[j][e];
   __syncthreads();
-  for (int e = threadIdx.x; e < A.tokens * kFewRows; e += blockDim.x) {
+  constexpr int kOutputs = 8 * GROUPS * kFewRows;
+  if (ranks > 1) {
+    // each CTA adds up its warps, then takes its share of the outputs and adds up the CTAs
+    for (int e = threadIdx.x; e < kOutputs; e += blockDim.x) {
+      float y = 0.0f;
+      for (int w = 0; w < warps; ++w) y += s_part[w * kOutputs + e];
+      s_part[e] = y;                         // (only this thread reads or writes column e)
+    }
+    tc::cluster_sync();
+  }
+  for (int e = threadIdx.x + rank * static_cast<int>(blockDim.x); e < A.tokens * kFewRows; e += ranks * static_cast<int>(blockDim.x)) {
     const int n = n0 + (e & (kFewRows - 1)), token = e / kFewRows;
     if (n >= A.n_out) continue;
     float y = 0.0f;
-    for (int w = 0; w < warps; ++w) y += s_part[w * 8 * GROUPS * kFewRows + e];
+    if (ranks > 1) {
+      for (int r = 0; r < ranks; ++r) {
+        float part;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(tc::map_to_cta(tc::smem_u32(s_part + e), r)) : "memory");
+        y += part;
+      }
+    } else {
+      for (int w = 0; w < warps; ++w) y += s_part[w * kOutputs + e];
+    }
     if (A.bias != nullptr) y += bf16_bits_to_float(ld_global(A.bias + n));
     if (A.act == BSP_ACT_GELU) {
       float unused = 0.0f;
@@ -135,23 +199,61 @@ linear_few_kernel(FewArgs A) {
     }
     A.Y[static_cast<size_t>(token) * A.ldy + n] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
   }
+  if (ranks > 1) {                           // no CTA leaves while another may read its sums
+    tc::cluster_arrive_relaxed();
+    tc::cluster_wait();
+  }
 }
 
 }  // namespace
 
 namespace fp8 {
 
+namespace {
+
+template <bool kReady, int FMT>
+int launch_few_of(FewArgs A, cudaStream_t s) {
+  const int n_out = A.n_out, k_in = A.k_in, tokens = A.tokens;
+  const int blocks = blocks_of(k_in), tiles = (n_out - 1) / kFewRows + 1;
+  int ranks = 1;
+  while (ranks < 4 && tiles * ranks * 2 <= kFewCtas && blocks / (ranks * 2) >= kFewLeastBlocks) ranks *= 2;
+  const int each = (blocks - 1) / ranks + 1, warps = each < kFewMaxWarps ? each : kFewMaxWarps;
+  const int groups = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4;
+  auto kernel = groups == 1   ? linear_few_kernel<1, kReady, FMT>
+                : groups == 2 ? linear_few_kernel<2, kReady, FMT>
+                              : linear_few_kernel<4, kReady, FMT>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles) * ranks);
+  cfg.blockDim = dim3(32 * warps);
+  cfg.dynamicSmemBytes = sizeof(float) * warps * 8 * groups * kFewRows;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ranks;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ranks > 1 ? 2 : 1;
+  BSP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, A));
+  return BSP_OK;
+}
+
+}  // namespace
+
 bool few_tokens_ok(const void* Wq, int ldw, int tokens) { return tokens <= kFewTokens && aligned_to(Wq, 16) && ldw % 16 == 0; }
 
 int launch_few(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* X, int tokens, int ldx, const void* bias, int act,
                void* Y, int ldy, cudaStream_t s) {
-  const FewArgs A{static_cast<const uint8_t*>(Wq), ldw, WS, ldws, n_out, k_in, static_cast<const uint16_t*>(X), tokens, ldx,
-                  aligned_to(X, 16) && ldx % 8 == 0, static_cast<const uint16_t*>(bias), act, static_cast<uint16_t*>(Y), ldy};
-  const int blocks = blocks_of(k_in), warps = blocks < kFewMaxWarps ? blocks : kFewMaxWarps;
-  const int groups = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4;
-  auto kernel = groups == 1 ? linear_few_kernel<1> : groups == 2 ? linear_few_kernel<2> : linear_few_kernel<4>;
-  BSP_CUDA_TRY(launch_pdl(kernel, dim3((n_out - 1) / kFewRows + 1), dim3(32 * warps), sizeof(float) * warps * 8 * groups * kFewRows, s, A));
-  return BSP_OK;
+  return launch_few_of<false, BSP_FP8_E4M3>(FewArgs{static_cast<const uint8_t*>(Wq), ldw, WS, ldws, n_out, k_in, X, tokens, ldx,
+                                                    aligned_to(X, 16) && ldx % 8 == 0, nullptr, 0, static_cast<const uint16_t*>(bias), act,
+                                                    static_cast<uint16_t*>(Y), ldy}, s);
+}
+int launch_few_ready(const Product& p, cudaStream_t s) {
+  const FewArgs A{p.B.q, p.B.ld, p.B.s, static_cast<int>(p.B.s_row), p.B.rows, p.contraction, p.A.q, p.A.rows, p.A.ld, 1, p.A.s, static_cast<int>(p.A.s_row),
+                  p.bias, p.act, p.Y, p.ldy};
+  return p.A.fmt == BSP_FP8_E4M3 ? launch_few_of<true, BSP_FP8_E4M3>(A, s) : launch_few_of<true, BSP_FP8_E5M2>(A, s);
 }
 
 }  // namespace fp8

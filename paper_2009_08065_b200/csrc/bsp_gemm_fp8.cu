@@ -290,6 +290,9 @@ __device__ __forceinline__ bool epilogue_agree(bool ok) {
   return r != 0u;
 }
 
+// The value is computed before anything that follows, not where it is first used.
+__device__ __forceinline__ void keep_here(int& x) { asm volatile("" : "+r"(x)); }
+
 template <bool kAMn, bool kBMn>
 __global__ void __launch_bounds__(kFp8Threads, 1)
 gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -341,9 +344,13 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const int k_blocks = blocks_of(P.contraction);
   const int accs = pair_accumulators(w);
   const int tiles_b = (w + 127) >> 7;                  // sets of 128 rows of B with scales
-  pdl_wait();
-  pdl_launch_dependents();
-  cluster_wait();                // and so do the other's, before anything signals across the pair
+  // Before this returns nothing of global memory is touched, and nothing signalled across the pair.  Each role calls it where it has computed
+  // all it can: the kernel before is mostly still running, and what comes behind it costs up to 0.5 us in instructions that are not cached yet.
+  auto begin_work = [&] {
+    pdl_wait();
+    pdl_launch_dependents();
+    cluster_wait();              // the other CTA's barriers exist, and its tensor memory is allocated
+  };
 
   if (warp == 0 || warp == 11) {
     // ---------------------------------------------------------------- TMA producers (both CTAs): warp 0 of A, warp 11 of B
@@ -356,8 +363,14 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
+    auto first_row = [&](int tile) {
+      return for_a ? (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM : (tile % n_tiles) * w + static_cast<int>(rank) * (w / 2);
+    };
+    int row0 = first_row(pair);
+    keep_here(row0);
+    begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
-      const int row0 = for_a ? (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM : (tile % n_tiles) * w + static_cast<int>(rank) * (w / 2);
+      if (tile != pair) row0 = first_row(tile);
       for (int kb = 0; kb < k_blocks; ++kb) {
         if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, P.status)) { ok = false; break; }
         tma_load_pair(smem_base + stage * kPairStage + at, map, mn ? row0 : kb * kBlock, mn ? kb * kBlock : row0, leader_full + 8u * stage,
@@ -378,8 +391,15 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     int slot = 0;
     uint32_t phase = 0;
     bool ok = true;
+    int m0 = (pair / n_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0 = (pair % n_tiles) * w;
+    keep_here(m0);
+    keep_here(n0);
+    begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
-      const int m0 = (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0 = (tile % n_tiles) * w;
+      if (tile != pair) {
+        m0 = (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM;
+        n0 = (tile % n_tiles) * w;
+      }
       for (int kb = 0; kb < k_blocks;) {
         const bool begin = tile == pair && kb == 0;
         const int n = min(begin ? 4 : 4 * kSlotGroups, k_blocks - kb);
@@ -417,6 +437,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     uint32_t phase = 0, slot_phase = 0, scale_buf = 0, acc_phases = 0;
     int acc = 0;
     bool ok = true;
+    begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
       if (!mbar_wait_warp(acc_empty_bar(acc), ((acc_phases >> acc) & 1u) ^ 1u, P.status)) { ok = false; break; }
       tcgen05_fence_after();
@@ -454,7 +475,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       if (accs == 2) acc ^= 1;
     }
     if (!ok && lane == 0) record_timeout(P.status, timed_out);
-  } else if (warp >= 2) {                              // (warp 1 of the other CTA has nothing to do)
+  } else if (warp >= 2) {
     // ---------------------------------------------------------------- epilogue of this CTA's 128 rows
     const int number = warp < 10 ? warp - 2 : warp - 4;          // 0 to 11
     const int group = number >> 2;
@@ -464,16 +485,19 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     uint32_t acc_phases = 0, bias_buf = 0;
     int acc = 0;
     bool ok = true;
-    for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
-      const int m0 = (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0 = (tile % n_tiles) * w;
+    // The first turn works on no tile: it brings the body's instructions to the caches (1500 cycles of the first piece) while there is
+    // nothing else to do, and stores nothing.
+    for (int tile = pair - n_pairs; tile < total_tiles && ok; tile += n_pairs) {
+      const bool dry = tile < pair;
+      const int m0 = dry ? rows : (tile / n_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0 = dry ? 0 : (tile % n_tiles) * w;
       for (int c = epi_tid; c < w; c += 32 * kEpiWarps)
-        s_bias[bias_buf * kPairMaxW + c] = (P.bias != nullptr && n0 + c < cols) ? ld_global(P.bias + n0 + c) : static_cast<uint16_t>(0);
+        s_bias[bias_buf * kPairMaxW + c] = (P.bias != nullptr && !dry && n0 + c < cols) ? ld_global(P.bias + n0 + c) : static_cast<uint16_t>(0);
       epilogue_meet();
       // all epilogue threads take the same decision, so nobody is left alone at a named barrier below
-      if (!epilogue_agree(mbar_wait(acc_full_bar(acc), (acc_phases >> acc) & 1u, P.status))) { ok = false; break; }
+      if (!epilogue_agree(dry || mbar_wait(acc_full_bar(acc), (acc_phases >> acc) & 1u, P.status))) { ok = false; break; }
       tcgen05_fence_after();
       const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(acc * w);
-      const int pieces = (min(w, cols - n0) + kEpiCols - 1) / kEpiCols;
+      const int pieces = dry ? kEpiGroups : (min(w, cols - n0) + kEpiCols - 1) / kEpiCols;
       // (the last piece of a tile whose width is no multiple of 32 begins early: both write the same values)
       auto first_col = [&](int pc) { return min(pc * kEpiCols, w - kEpiCols); };
       // One body for all pieces, the next one's accumulators on their way while a piece is finished.  (Unrolled, with all pieces in registers
@@ -492,6 +516,10 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         finish_piece(P, v, smem_u32(s_bias + bias_buf * kPairMaxW + first_col(pc)), buf, m0 + quad * 32, n0 + first_col(pc), lane);
         tmem_load_wait();
       }
+      if (dry) {
+        begin_work();
+        continue;
+      }
       // (the last accumulators are not waited for again: no arrival that could come when the leader has left)
       if (tile + accs * n_pairs < total_tiles) {
         tcgen05_fence_before();
@@ -503,6 +531,8 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       bias_buf ^= 1u;
     }
     if (!ok && lane == 0) record_timeout(P.status, timed_out);
+  } else {
+    begin_work();                                       // (warp 1 of the other CTA has nothing else to do)
   }
 
   tcgen05_fence_before();
@@ -525,14 +555,13 @@ bool make_map8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t oute
   const cuuint64_t strides[1] = {ld};
   const cuuint32_t box[2] = {kBlock, box_outer};
   const cuuint32_t elem[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// The driver's encoder wants a current context, which a thread that has only asked the runtime for facts does not have.
-bool make_current() {
-  int device = 0;
-  return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess;
+  auto encode = [&] {
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (encode()) return true;
+  int device = 0;            // (a thread without a current context: see make_map)
+  return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
 }
 
 template <bool kAMn, bool kBMn>
@@ -540,7 +569,6 @@ int launch_pair(const Product& p, int w, TcDevice* dev, cudaStream_t s) {
   static OncePerDevice once;
   BSP_TRY(allow_dynamic_smem(once, gemm_fp8_pair_kernel<kAMn, kBMn>, kPairSmem));
   CUtensorMap map_a, map_b;
-  if (!make_current()) return BSP_ERR_CUDA;
   const int b_rows = kBMn ? kBlock : w / 2;
   if (!(kAMn ? make_map8(&map_a, p.A.q, p.A.rows, p.contraction, p.A.ld, kBlock) : make_map8(&map_a, p.A.q, p.contraction, p.A.rows, p.A.ld, kBlockM)) ||
       !(kBMn ? make_map8(&map_b, p.B.q, p.B.rows, p.contraction, p.B.ld, kBlock) : make_map8(&map_b, p.B.q, p.contraction, p.B.rows, p.B.ld, b_rows)))

@@ -87,6 +87,10 @@ Operand weight_operand(const void* Wq, int ldw, const uint8_t* WS, int ldws, int
   return Operand{static_cast<const uint8_t*>(Wq), n_out, ldw, 0, BSP_FP8_E4M3, WS, ldws, 1, 7};
 }
 constexpr int kMostInputs = 0x7fffffff / 16 * 16;
+// Few tokens and a large weight: the CTAs of 16 outputs would each bring all tokens to 8 bits (13 tokens, 4096 x 4096: in one launch 10.8 us, quantised
+// first 9.4; 4096 x 1024: 3.6 and 4.4), and from some 16 tokens on the pairs are faster (32 tokens, 4096 x 4096: 18.6, 14.5, and 12.4 by pairs; 1024 x
+// 4096: 6.5, 6.8 and 11.8).
+bool large_weight(int n_out, int k_in) { return static_cast<long long>(n_out) * k_in >= (8ll << 20); }
 int row_pitch(int k_in) { return (k_in - 1) / 16 * 16 + 16; }
 
 }  // namespace
@@ -101,6 +105,8 @@ extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* 
   if (ldx < k_in || ldxs < blocks_of(k_in) || ldy < n_out) return BSP_ERR_SHAPE;
   const Product p{Operand{static_cast<const uint8_t*>(Xq), tokens, ldx, 0, fmt, XS, ldxs, 1, 0}, weight_operand(Wq, ldw, WS, ldws, n_out), k_in,
                   static_cast<uint16_t*>(Y), ldy, static_cast<const uint16_t*>(bias), act, nullptr, 1};
+  if (few_tokens_ok(Wq, ldw, tokens) && aligned_to(Xq, 16) && ldx % 16 == 0 && (tokens <= 16 || !large_weight(n_out, k_in)))
+    return launch_few_ready(p, static_cast<cudaStream_t>(stream));
   return run_product(p, static_cast<cudaStream_t>(stream));
 }
 
@@ -123,7 +129,7 @@ extern "C" int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ld
   size_t need = 0;
   BSP_TRY(bsp_linear_fp8_ws_bytes(tokens, k_in, &need));
   if (ws_bytes < need) return BSP_ERR_WORKSPACE;
-  if (few_tokens_ok(Wq, ldw, tokens))
+  if (few_tokens_ok(Wq, ldw, tokens) && (tokens <= 8 || !large_weight(n_out, k_in)))
     return launch_few(Wq, ldw, WS, ldws, n_out, k_in, X, tokens, ldx, bias, act, Y, ldy, static_cast<cudaStream_t>(stream));
   uint8_t* Q = static_cast<uint8_t*>(ws);
   uint8_t* S = Q + static_cast<size_t>(tokens) * row_pitch(k_in);
