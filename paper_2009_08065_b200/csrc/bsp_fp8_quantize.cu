@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "bsp_fp8.cuh"
+#include "bsp_tc.cuh"
 
 namespace bsp {
 using namespace fp8;
@@ -32,9 +33,23 @@ struct QuantArgs {
   int wide_in, wide_out;     // 16-byte loads; stores of 16 (2), 8 (1) or single bytes (0)
 };
 
-// kRows: along the rows only.  kBoth: along the columns, column sums, and along the rows where asked for.  kTile: one scale for the tile.
-enum class QuantKind { kRows, kBoth, kTile };
-
+// A pair of values times a pair of multipliers, as 8 bits.
+template <int FMT>
+__device__ __forceinline__ uint32_t pair_times(unsigned long long v, unsigned long long m) {
+  float lo, hi;
+  unsigned long long p;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p) : "l"(v), "l"(m));
+  tc::unpack_f32x2(p, lo, hi);
+  return to_fp8x2<FMT>(lo, hi);
+}
+__device__ __noinline__ void store_some(uint8_t* dst, uint4 q, int n) {
+  unsigned long long v = q.x | (static_cast<unsigned long long>(q.y) << 32);
+#pragma unroll 1
+  for (int i = 0; i < n; ++i, v >>= 8) {
+    if (i == 8) v = q.z | (static_cast<unsigned long long>(q.w) << 32);
+    dst[i] = static_cast<uint8_t>(v);
+  }
+}
 // Sixteen bytes, of which n exist.
 __device__ __forceinline__ void store_sixteen(uint8_t* dst, const uint32_t (&q)[4], int n, int wide) {
   if (wide == 2 && n == 16) {
@@ -42,28 +57,29 @@ __device__ __forceinline__ void store_sixteen(uint8_t* dst, const uint32_t (&q)[
   } else if (wide >= 1 && n >= 8 && (n & 7) == 0) {
     *reinterpret_cast<uint2*>(dst) = make_uint2(q[0], q[1]);
     if (n == 16) *reinterpret_cast<uint2*>(dst + 8) = make_uint2(q[2], q[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < n) dst[i] = static_cast<uint8_t>(q[i >> 2] >> (8 * (i & 3)));
+  } else if (n > 0) {
+    store_some(dst, make_uint4(q[0], q[1], q[2], q[3]), n);
   }
 }
 
-template <int FMT, QuantKind KIND>
-__global__ void __launch_bounds__(kQuantThreads)
-quantize_kernel(QuantArgs A) {
-  __shared__ uint32_t s_max[8][64];          // [warp][pair of columns]
-  __shared__ __align__(16) float s_inv[128];
-  __shared__ float s_sum[8][128];
-  const int warp = threadIdx.x >> 5, l = threadIdx.x & 7, slot = threadIdx.x >> 3;   // eight threads to a row
-  const int r0 = blockIdx.y * kBlock, c0 = blockIdx.x * kBlock, c = c0 + 16 * l;
-  const int n = max(0, min(16, A.cols - c));   // of this thread's columns, those that exist
-  pdl_wait();
-  pdl_launch_dependents();
-  uint32_t x[4][8];
+// Up to eight values one by one.  (A loop, and so below: unrolled into every place that may need it, this was most of the kernel's code,
+// and in a short launch every instruction is fetched for the first time.)
+__device__ __noinline__ uint4 load_some(const uint16_t* src, int n) {
+  unsigned long long lo = 0ull, hi = 0ull;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    const unsigned long long v = ld_global(src + j);
+    if (j < 4) lo |= v << (16 * j);
+    else hi |= v << (16 * (j - 4));
+  }
+  return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32));
+}
+// A thread's rows x 16 columns of the tile, as pairs.
+template <int ROWS>
+__device__ __forceinline__ void load_tile(const QuantArgs& A, int r0, int c, int n, uint32_t (&x)[ROWS][8]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {              // rows slot, slot + 32, ...
-    const int r = r0 + slot + 32 * i;
+  for (int i = 0; i < ROWS; ++i) {           // evenly spread from this thread's first one on
+    const int r = r0 + kBlock / ROWS * i;
     const uint16_t* src = A.X + static_cast<size_t>(r) * A.ldx + c;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -72,65 +88,85 @@ quantize_kernel(QuantArgs A) {
         if (A.wide_in && n >= 8 * h + 8) {
           v = ld_global(reinterpret_cast<const uint4*>(src + 8 * h));
         } else if (n > 8 * h) {
-          uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (8 * h + j < n) w[j >> 1] |= static_cast<uint32_t>(ld_global(src + 8 * h + j)) << (16 * (j & 1));
-          v = make_uint4(w[0], w[1], w[2], w[3]);
+          v = load_some(src + 8 * h, min(8, n - 8 * h));
         }
       }
       x[i][4 * h] = v.x; x[i][4 * h + 1] = v.y; x[i][4 * h + 2] = v.z; x[i][4 * h + 3] = v.w;
     }
   }
-  if (KIND == QuantKind::kTile) {
-    uint32_t m = 0u;
+}
+// Largest magnitude of a row of the tile, by its eight threads.
+__device__ __forceinline__ uint32_t row_max(const uint32_t (&x)[8]) {
+  uint32_t m = abs_max2(x[0], x[1]);
+#pragma unroll
+  for (int j = 2; j < 8; ++j) m = abs_max2(m, x[j]);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return abs_max_of(m);
+}
+
+// Along the rows, or (kTile) with one scale for the tile.
+template <int FMT, bool kTile>
+__global__ void __launch_bounds__(kQuantThreads)
+quantize_kernel(QuantArgs A) {
+  __shared__ uint32_t s_max[8];
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 7, slot = threadIdx.x >> 3;   // eight threads to a row
+  const int r0 = blockIdx.y * kBlock + slot, c = blockIdx.x * kBlock + 16 * l;
+  const int n = max(0, min(16, A.cols - c));   // of this thread's columns, those that exist
+  pdl_wait();
+  pdl_launch_dependents();
+  uint32_t x[4][8];
+  load_tile(A, r0, c, n, x);
+  uint32_t tile = 0u;
+  if (kTile) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) m = abs_max2(m, x[i][j]);
-    m = __reduce_max_sync(0xffffffffu, abs_max_of(m));
-    if ((threadIdx.x & 31) == 0) s_max[warp][0] = m;
+      for (int j = 0; j < 8; ++j) tile = abs_max2(tile, x[i][j]);
+    tile = __reduce_max_sync(0xffffffffu, abs_max_of(tile));
+    if ((threadIdx.x & 31) == 0) s_max[warp] = tile;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, s_max[w][0]);
+    for (int w = 0; w < 8; ++w) tile = max(tile, s_max[w]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + 32 * i;
     float inv;
-    const uint32_t byte = block_scale<FMT>(m, inv);
-    if (threadIdx.x == 0) A.s_row[static_cast<size_t>(blockIdx.y) * A.lds_row + blockIdx.x] = static_cast<uint8_t>(byte);
+    const uint32_t byte = block_scale<FMT>(kTile ? tile : row_max(x[i]), inv);
+    if (r >= A.rows) continue;
+    if (kTile ? threadIdx.x == 0 && i == 0 : l == 0)
+      A.s_row[static_cast<size_t>(kTile ? blockIdx.y : r) * A.lds_row + blockIdx.x] = static_cast<uint8_t>(byte);
+    uint32_t q[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + slot + 32 * i;
-      if (r >= A.rows) continue;
-      uint32_t q[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = four_to_fp8<FMT>(x[i][2 * j], x[i][2 * j + 1], inv, inv, inv, inv);
-      store_sixteen(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
-    }
-    return;
+    for (int j = 0; j < 4; ++j) q[j] = four_to_fp8<FMT>(x[i][2 * j], x[i][2 * j + 1], inv, inv, inv, inv);
+    store_sixteen(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
   }
-  if (KIND == QuantKind::kRows || A.q_row != nullptr) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + slot + 32 * i;
-      uint32_t m = abs_max2(x[i][0], x[i][1]);
-#pragma unroll
-      for (int j = 2; j < 8; ++j) m = abs_max2(m, x[i][j]);
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, o));
-      float inv;
-      const uint32_t byte = block_scale<FMT>(abs_max_of(m), inv);
-      if (r >= A.rows) continue;
-      if (l == 0) A.s_row[static_cast<size_t>(r) * A.lds_row + blockIdx.x] = static_cast<uint8_t>(byte);
-      uint32_t q[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = four_to_fp8<FMT>(x[i][2 * j], x[i][2 * j + 1], inv, inv, inv, inv);
-      store_sixteen(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
-    }
-  }
-  if (KIND == QuantKind::kRows) return;
+}
+
+// Along the columns, and column sums and along the rows where they are asked for.  Bound by issue beside HBM (8 instructions a value):
+// every pair is unpacked once for both forms and multiplied as a pair.  4096 x 4096 15.6 us (10.3 of HBM), with column sums 17.5; 512 threads with
+// two rows each were no faster.
+template <int FMT>
+__global__ void __launch_bounds__(kQuantThreads, 4)
+quantize_both_kernel(QuantArgs A) {
+  constexpr int kRows = kBlock * 8 / kQuantThreads, kWarps = kQuantThreads / 32, kStep = kBlock / kRows;
+  __shared__ uint32_t s_max[kWarps][64];     // [warp][pair of columns]
+  __shared__ __align__(16) float s_inv[128];
+  __shared__ __align__(16) float s_sum[kWarps][128];
+  const int warp = threadIdx.x >> 5, l = threadIdx.x & 7, slot = threadIdx.x >> 3;
+  const int r0 = blockIdx.y * kBlock + slot, c0 = blockIdx.x * kBlock, c = c0 + 16 * l;
+  const int n = max(0, min(16, A.cols - c));
+  pdl_wait();
+  pdl_launch_dependents();
+  uint32_t x[kRows][8];
+  load_tile(A, r0, c, n, x);
   if (A.q_col != nullptr) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t m = abs_max2(abs_max2(x[0][j], x[1][j]), abs_max2(x[2][j], x[3][j]));
+      uint32_t m = x[0][j];
+#pragma unroll
+      for (int i = 1; i < kRows; ++i) m = abs_max2(m, x[i][j]);
       m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 8));
       m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 16));
       if ((threadIdx.x & 24) == 0) s_max[warp][8 * l + j] = m;
@@ -141,7 +177,7 @@ quantize_kernel(QuantArgs A) {
     for (int j = 0; j < 8; ++j) {
       float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kRows; ++i) {
         lo += __uint_as_float(x[i][j] << 16);
         hi += __uint_as_float(x[i][j] & 0xffff0000u);
       }
@@ -150,10 +186,7 @@ quantize_kernel(QuantArgs A) {
         lo += __shfl_xor_sync(0xffffffffu, lo, o);
         hi += __shfl_xor_sync(0xffffffffu, hi, o);
       }
-      if ((threadIdx.x & 24) == 0) {
-        s_sum[warp][16 * l + 2 * j] = lo;
-        s_sum[warp][16 * l + 2 * j + 1] = hi;
-      }
+      if ((threadIdx.x & 24) == 0) *reinterpret_cast<float2*>(&s_sum[warp][16 * l + 2 * j]) = make_float2(lo, hi);
     }
   }
   __syncthreads();
@@ -161,7 +194,7 @@ quantize_kernel(QuantArgs A) {
     if (A.q_col != nullptr) {
       uint32_t m = 0u;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) m = abs_max2(m, s_max[w][threadIdx.x]);
+      for (int w = 0; w < kWarps; ++w) m = abs_max2(m, s_max[w][threadIdx.x]);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int at = 2 * threadIdx.x + u;
@@ -174,36 +207,55 @@ quantize_kernel(QuantArgs A) {
   } else if (A.partial != nullptr && threadIdx.x >= 128 && c0 + static_cast<int>(threadIdx.x) - 128 < A.cols) {
     float t = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t += s_sum[w][threadIdx.x - 128];
+    for (int w = 0; w < kWarps; ++w) t += s_sum[w][threadIdx.x - 128];
     A.partial[static_cast<size_t>(blockIdx.y) * A.cols + c0 + threadIdx.x - 128] = t;
   }
-  if (A.q_col == nullptr) return;
+  uint32_t top[kRows];
+  if (A.q_row != nullptr) {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) top[i] = row_max(x[i]);
+  }
   __syncthreads();
-  float4 inv[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) inv[j] = reinterpret_cast<const float4*>(s_inv)[4 * l + j];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = r0 + slot + 32 * i;
+  for (int i = 0; i < kRows; ++i) {
+    const int r = r0 + kStep * i;
     if (r >= A.rows) continue;
-    uint32_t q[4];
+    float inv = 0.0f;
+    if (A.q_row != nullptr) {
+      const uint32_t byte = block_scale<FMT>(top[i], inv);
+      if (l == 0) A.s_row[static_cast<size_t>(r) * A.lds_row + blockIdx.x] = static_cast<uint8_t>(byte);
+    }
+    const unsigned long long along = tc::pack_f32x2(inv, inv);
+    uint32_t q[4], p[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q[j] = four_to_fp8<FMT>(x[i][2 * j], x[i][2 * j + 1], inv[j].x, inv[j].y, inv[j].z, inv[j].w);
-    store_sixteen(A.q_col + static_cast<size_t>(r) * A.ld_col + c, q, n, A.wide_out);
+    for (int j = 0; j < 4; ++j) {
+      const float4 down = A.q_col != nullptr ? reinterpret_cast<const float4*>(s_inv)[4 * l + j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const unsigned long long v0 = tc::pack_f32x2(__uint_as_float(x[i][2 * j] << 16), __uint_as_float(x[i][2 * j] & 0xffff0000u));
+      const unsigned long long v1 = tc::pack_f32x2(__uint_as_float(x[i][2 * j + 1] << 16), __uint_as_float(x[i][2 * j + 1] & 0xffff0000u));
+      q[j] = pair_times<FMT>(v0, along) | (pair_times<FMT>(v1, along) << 16);
+      p[j] = pair_times<FMT>(v0, tc::pack_f32x2(down.x, down.y)) | (pair_times<FMT>(v1, tc::pack_f32x2(down.z, down.w)) << 16);
+    }
+    if (A.q_row != nullptr) store_sixteen(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
+    if (A.q_col != nullptr) store_sixteen(A.q_col + static_cast<size_t>(r) * A.ld_col + c, p, n, A.wide_out);
   }
 }
 
-// The blocks' column sums, added in their order.
-__global__ void __launch_bounds__(128)
+// The blocks' column sums: four runs of blocks side by side, and the runs in their order.
+__global__ void __launch_bounds__(512)
 column_sums_kernel(const float* partial, int blocks, int cols, float* out) {
-  const int c = blockIdx.x * 128 + threadIdx.x;
+  __shared__ float s_sum[4][128];
+  const int c = blockIdx.x * 128 + (threadIdx.x & 127), run = threadIdx.x >> 7;
+  const int each = (blocks + 3) / 4, begin = run * each, end = min(blocks, begin + each);
   pdl_wait();
   pdl_launch_dependents();
-  if (c >= cols) return;
   float t = 0.0f;
+  if (c < cols) {
 #pragma unroll 8
-  for (int b = 0; b < blocks; ++b) t += ld_global(partial + static_cast<size_t>(b) * cols + c);
-  out[c] = t;
+    for (int b = begin; b < end; ++b) t += ld_global(partial + static_cast<size_t>(b) * cols + c);
+  }
+  s_sum[run][threadIdx.x & 127] = t;
+  __syncthreads();
+  if (run == 0 && c < cols) out[c] = s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x] + s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x];
 }
 
 int wide_stores(const void* q, int ld) { return aligned_to(q, 16) && ld % 16 == 0 ? 2 : aligned_to(q, 8) && ld % 8 == 0 ? 1 : 0; }
@@ -235,11 +287,11 @@ extern "C" int bsp_fp8_quantize(const void* X, int rows, int cols, int ldx, int 
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const dim3 grid(blocks_of(cols), blocks_of(rows));
   const bool rows_only = Qc == nullptr && col_sums == nullptr;
-  auto kernel = fmt == BSP_FP8_E4M3 ? (rows_only ? quantize_kernel<BSP_FP8_E4M3, QuantKind::kRows> : quantize_kernel<BSP_FP8_E4M3, QuantKind::kBoth>)
-                                    : (rows_only ? quantize_kernel<BSP_FP8_E5M2, QuantKind::kRows> : quantize_kernel<BSP_FP8_E5M2, QuantKind::kBoth>);
+  auto kernel = fmt == BSP_FP8_E4M3 ? (rows_only ? quantize_kernel<BSP_FP8_E4M3, false> : quantize_both_kernel<BSP_FP8_E4M3>)
+                                    : (rows_only ? quantize_kernel<BSP_FP8_E5M2, false> : quantize_both_kernel<BSP_FP8_E5M2>);
   BSP_CUDA_TRY(launch_pdl(kernel, grid, dim3(kQuantThreads), 0, s, A));
   if (col_sums != nullptr)
-    BSP_CUDA_TRY(launch_pdl(column_sums_kernel, dim3(blocks_of(cols)), dim3(128), 0, s, A.partial, static_cast<int>(grid.y), cols, col_sums));
+    BSP_CUDA_TRY(launch_pdl(column_sums_kernel, dim3(blocks_of(cols)), dim3(512), 0, s, A.partial, static_cast<int>(grid.y), cols, col_sums));
   return BSP_OK;
 }
 
@@ -254,7 +306,7 @@ extern "C" int bsp_fp8_quantize_weight(const void* W, int n_out, int k_in, int l
   A.q_row = static_cast<uint8_t*>(Q); A.ld_row = ldq; A.s_row = S; A.lds_row = lds;
   A.wide_in = aligned_to(W, 16) && ldw % 8 == 0;
   A.wide_out = wide_stores(Q, ldq);
-  BSP_CUDA_TRY(launch_pdl(quantize_kernel<BSP_FP8_E4M3, QuantKind::kTile>, dim3(blocks_of(k_in), blocks_of(n_out)), dim3(kQuantThreads), 0,
+  BSP_CUDA_TRY(launch_pdl(quantize_kernel<BSP_FP8_E4M3, true>, dim3(blocks_of(k_in), blocks_of(n_out)), dim3(kQuantThreads), 0,
                           static_cast<cudaStream_t>(stream), A));
   return BSP_OK;
 }
