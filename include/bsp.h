@@ -521,7 +521,9 @@ int bsp_linear_tune(const bsp_linear_call* call, int reps, int* best_route, floa
  * Outputs may have any alignment; they are stored fastest where they are 16-byte aligned with rows and leading dimensions of a
  * multiple of 8.  Bounded waits as bsp_linear_planned: check bsp_linear_status.
  * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE (leading dimension too small, block does not divide n_out), BSP_ERR_WORKSPACE,
- * BSP_ERR_UNSUPPORTED (bsp_fp8_quantize*: more than 65535 * 128 rows; bsp_linear_fp8*: more than 2^31 - 16 inputs). */
+ * BSP_ERR_UNSUPPORTED (a size beyond 2^31 - 512; bsp_fp8_quantize*: more than 65535 * 128 rows).
+ * The kernel is chosen by size, so a row's last bits may differ between numbers of tokens; the same call gives the same bits.  Calls that
+ * may run at the same time need a ws each. */
 typedef enum { BSP_FP8_E4M3 = 0, BSP_FP8_E5M2 = 1 } bsp_fp8_format;
 int bsp_fp8_quantize(const void* X, int rows, int cols, int ldx, int fmt, void* Q, int ldq, uint8_t* S, int lds, void* Qc, int ldqc,
                      uint8_t* Sc, int ldsc, float* col_sums, void* ws, size_t ws_bytes, void* stream);
@@ -551,10 +553,11 @@ int bsp_linear_fp8_backward_weight(const void* dYq, int ldy, const uint8_t* dYS,
  *     16 random bits each, a hash of (seed, step, number of the job in the array, position in the tensor): the same call
  *     gives the same bits.  A positive v is never rounded to zero.  A block whose new moments hold an infinity or a NaN becomes NaN.
  * grad_scale: device float that multiplies every gradient (clipping), or NULL.  step >= 1; if step_dev is not NULL the step is read from there
- * instead, so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step.
+ * instead (it has to be at least 1 when the call runs), so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step.
  * Any shape and alignment; 16-byte accesses where pointers and leading dimensions allow them.  No two jobs may share memory that either writes.
- * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE, BSP_ERR_UNSUPPORTED (a tensor of more than 2^41 weights); all jobs are checked before the
- * first launch. */
+ * Bounded waits (8-bit moments) as bsp_linear_planned: check bsp_linear_status.
+ * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE, BSP_ERR_UNSUPPORTED (more than 2^31 - 512 rows or columns, or 2^41 weights); all jobs are
+ * checked before the first launch. */
 typedef enum { BSP_GRAD_F32 = 0, BSP_GRAD_BF16 = 1 } bsp_grad_type;
 typedef struct bsp_adam_job {
   float* W; int rows, cols, ldw;

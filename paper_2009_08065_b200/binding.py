@@ -455,8 +455,12 @@ class AdamJob:
 def make_adam_job_array(jobs):
     """The host descriptor array for bsp_masked_adam_step_batched; build it once and reuse it while the tensors stay."""
     arr = (_AdamJob * len(jobs))()
+    arr.device = jobs[0].W.device.index if jobs else None
     for a, j in zip(arr, jobs):
         shape = tuple(j.W.shape)
+        for t in (j.W, j.grad, j.m, j.v, j.m_scale, j.v_scale, j.keep, j.W_bf16):
+            if t is not None and t.device != j.W.device or j.W.device.index != arr.device:
+                raise ValueError("the tensors of a call are on different devices")
         for t in (j.grad, j.m, j.v, j.W_bf16):
             if t is not None and tuple(t.shape) != shape:
                 raise ValueError(f"tensors of one job have shapes {shape} and {tuple(t.shape)}")
@@ -491,6 +495,9 @@ def bsp_masked_adam_step_batched(jobs, beta1: float, beta2: float, eps: float, s
     arr = jobs if isinstance(jobs, ctypes.Array) else make_adam_job_array(jobs)
     if arr._type_ is not _AdamJob:
         raise ctypes.ArgumentError(f"expected an array made by make_adam_job_array, got {type(jobs).__name__}")
+    device = getattr(arr, "device", None)
+    if device is not None and device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {device}, the current one is {torch.cuda.current_device()}")
     _check(_native.masked_adam_step_batched(ctypes.addressof(arr), len(arr), beta1, beta2, eps, step, seed, grad_scale, step_dev,
                                             stream), "bsp_masked_adam_step_batched")
 

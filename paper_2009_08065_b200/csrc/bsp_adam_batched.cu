@@ -679,7 +679,7 @@ int make_job(const bsp_adam_job& a, uint32_t tensor, AdamJob* j, long long* ctas
   j->kb_magic = magic(blocks_of(a.cols));
   const long long groups = static_cast<long long>(a.rows) * blocks_of(a.cols);
   *ctas = (groups + kAdamGroups - 1) / kAdamGroups;
-  return *ctas > 0x3fffffffLL ? BSP_ERR_UNSUPPORTED : BSP_OK;
+  return *ctas > 0x3fffffffLL || a.rows > kMostSize || a.cols > kMostSize ? BSP_ERR_UNSUPPORTED : BSP_OK;
 }
 
 }  // namespace

@@ -26,6 +26,8 @@ struct Operand {
 };
 
 __host__ __device__ constexpr int blocks_of(int n) { return (n - 1) / kBlock + 1; }      // n >= 1 (up to the largest int)
+// Largest size in any direction: the kernels count up to a tile beyond it.
+constexpr int kMostSize = 0x7ffffe00;
 inline bool known_format(int fmt) { return fmt == BSP_FP8_E4M3 || fmt == BSP_FP8_E5M2; }
 
 #ifdef __CUDACC__

@@ -271,7 +271,7 @@ extern "C" int bsp_fp8_quantize(const void* X, int rows, int cols, int ldx, int 
   if ((Q == nullptr) != (S == nullptr) || (Qc == nullptr) != (Sc == nullptr)) return BSP_ERR_ARG;
   if (Q == nullptr && Qc == nullptr && col_sums == nullptr) return BSP_ERR_ARG;
   if (ldx < cols || (Q != nullptr && (ldq < cols || lds < blocks_of(cols))) || (Qc != nullptr && (ldqc < cols || ldsc < cols))) return BSP_ERR_SHAPE;
-  if (!grid_fits(rows)) return BSP_ERR_UNSUPPORTED;
+  if (!grid_fits(rows) || cols > kMostSize) return BSP_ERR_UNSUPPORTED;
   if (col_sums != nullptr) {
     if (ws == nullptr || !aligned_to(ws, 4) || !aligned_to(col_sums, 4)) return BSP_ERR_ARG;
     if (ws_bytes < sizeof(float) * static_cast<size_t>(blocks_of(rows)) * cols) return BSP_ERR_WORKSPACE;
@@ -299,7 +299,7 @@ extern "C" int bsp_fp8_quantize_weight(const void* W, int n_out, int k_in, int l
   using namespace bsp;
   if (W == nullptr || Q == nullptr || S == nullptr || n_out <= 0 || k_in <= 0 || !aligned_to(W, 2)) return BSP_ERR_ARG;
   if (ldw < k_in || ldq < k_in || lds < blocks_of(k_in)) return BSP_ERR_SHAPE;
-  if (!grid_fits(n_out)) return BSP_ERR_UNSUPPORTED;
+  if (!grid_fits(n_out) || k_in > kMostSize) return BSP_ERR_UNSUPPORTED;
   QuantArgs A = {};
   A.X = static_cast<const uint16_t*>(W);
   A.rows = n_out; A.cols = k_in; A.ldx = ldw;

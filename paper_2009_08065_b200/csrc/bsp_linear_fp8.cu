@@ -71,6 +71,7 @@ product_any_kernel(const __grid_constant__ AnyArgs args) {
 }
 
 int run_product(const Product& p, cudaStream_t s) {
+  if (p.A.rows > kMostSize || p.B.rows > kMostSize || p.contraction > kMostSize) return BSP_ERR_UNSUPPORTED;
   if (tensor_core_ok(p)) return launch_tensor_core(p, s);
   const long long tiles = static_cast<long long>((p.A.rows + kAnyTile - 1) / kAnyTile) * ((p.B.rows + kAnyTile - 1) / kAnyTile);
   if (tiles > 0x7fffffffLL) return BSP_ERR_UNSUPPORTED;
@@ -86,7 +87,6 @@ int check_weight(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out
 Operand weight_operand(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out) {
   return Operand{static_cast<const uint8_t*>(Wq), n_out, ldw, 0, BSP_FP8_E4M3, WS, ldws, 1, 7};
 }
-constexpr int kMostInputs = 0x7fffffff / 16 * 16;
 // Few tokens and a large weight: the CTAs of 16 outputs would each bring all tokens to 8 bits (13 tokens, 4096 x 4096: in one launch 10.8 us, quantised
 // first 9.4; 4096 x 1024: 3.6 and 4.4), and from some 16 tokens on the pairs are faster (32 tokens, 4096 x 4096: 18.6, 14.5, and 12.4 by pairs; 1024 x
 // 4096: 6.5, 6.8 and 11.8).
@@ -105,6 +105,7 @@ extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* 
   if (ldx < k_in || ldxs < blocks_of(k_in) || ldy < n_out) return BSP_ERR_SHAPE;
   const Product p{Operand{static_cast<const uint8_t*>(Xq), tokens, ldx, 0, fmt, XS, ldxs, 1, 0}, weight_operand(Wq, ldw, WS, ldws, n_out), k_in,
                   static_cast<uint16_t*>(Y), ldy, static_cast<const uint16_t*>(bias), act, nullptr, 1};
+  if (n_out > kMostSize || k_in > kMostSize) return BSP_ERR_UNSUPPORTED;
   if (few_tokens_ok(Wq, ldw, tokens) && aligned_to(Xq, 16) && ldx % 16 == 0 && (tokens <= 16 || !large_weight(n_out, k_in)))
     return launch_few_ready(p, static_cast<cudaStream_t>(stream));
   return run_product(p, static_cast<cudaStream_t>(stream));
@@ -113,7 +114,7 @@ extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* 
 extern "C" int bsp_linear_fp8_ws_bytes(int tokens, int k_in, size_t* bytes) {
   using namespace bsp;
   if (tokens <= 0 || k_in <= 0 || bytes == nullptr) return BSP_ERR_ARG;
-  if (k_in > kMostInputs) return BSP_ERR_UNSUPPORTED;
+  if (tokens > kMostSize || k_in > kMostSize) return BSP_ERR_UNSUPPORTED;
   *bytes = round_up(static_cast<size_t>(tokens) * (row_pitch(k_in) + blocks_of(k_in)), 256);
   return BSP_OK;
 }
@@ -129,6 +130,7 @@ extern "C" int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ld
   size_t need = 0;
   BSP_TRY(bsp_linear_fp8_ws_bytes(tokens, k_in, &need));
   if (ws_bytes < need) return BSP_ERR_WORKSPACE;
+  if (n_out > kMostSize) return BSP_ERR_UNSUPPORTED;
   if (few_tokens_ok(Wq, ldw, tokens) && (tokens <= 8 || !large_weight(n_out, k_in)))
     return launch_few(Wq, ldw, WS, ldws, n_out, k_in, X, tokens, ldx, bias, act, Y, ldy, static_cast<cudaStream_t>(stream));
   uint8_t* Q = static_cast<uint8_t*>(ws);

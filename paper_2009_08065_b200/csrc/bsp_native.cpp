@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,7 +28,7 @@ struct Matrix {
 // Positional arguments of one call; a failed conversion throws and ends as a Python exception.
 class Args {
  public:
-  Args(const char* name, PyObject* const* a, Py_ssize_t n, Py_ssize_t want) : a_(a) {
+  Args(const char* name, PyObject* const* a, Py_ssize_t n, Py_ssize_t want) : a_(a), n_(n) {
     TORCH_CHECK_TYPE(n == want, name, " takes ", want, " arguments, got ", n);
   }
   const at::Tensor& tensor(int i) const {
@@ -47,6 +48,14 @@ class Args {
     TORCH_CHECK_VALUE(t.dim() == 2 && t.stride(1) == 1, "expected a 2-D tensor with unit inner stride");
     const int64_t ld = t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
     return Matrix{t.data_ptr(), static_cast<int>(t.size(0)), static_cast<int>(t.size(1)), static_cast<int>(ld)};
+  }
+  // Every tensor on the current device, whose stream the call goes to.
+  void one_device() const {
+    const int current = static_cast<int>(c10::cuda::current_device());
+    for (Py_ssize_t i = 0; i < n_; ++i)
+      if (THPVariable_Check(a_[i]))
+        TORCH_CHECK_VALUE(tensor(static_cast<int>(i)).get_device() == current, "a tensor is on device ", tensor(static_cast<int>(i)).get_device(),
+                          ", the current one is ", current);
   }
   static void want_shape(const Matrix& m, int rows, int cols) {
     TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols, "expected a tensor of shape [", rows, ", ", cols, "], got [", m.rows, ", ", m.cols, "]");
@@ -102,6 +111,7 @@ class Args {
     return p;
   }
   PyObject* const* a_;
+  const Py_ssize_t n_;
 };
 
 template <class F>
@@ -339,6 +349,7 @@ NATIVE(linear_run) {
 // (X, fmt, Q, S, Qc, Sc, col_sums, ws, stream)
 NATIVE(fp8_quantize) {
   NATIVE_ARGS(fp8_quantize, 9);
+  A.one_device();
   const Matrix X = A.matrix(0), Q = A.matrix_like(2, X), S = A.scales(3, X.rows, blocks(X.cols));
   const Matrix Qc = A.matrix_like(4, X), Sc = A.scales(5, blocks(X.rows), X.cols);
   A.want_bytes(0, 2);
@@ -358,6 +369,7 @@ NATIVE(fp8_quantize) {
 // (W, Q, S, stream)
 NATIVE(fp8_quantize_weight) {
   NATIVE_ARGS(fp8_quantize_weight, 4);
+  A.one_device();
   const Matrix W = A.matrix(0), Q = A.matrix_like(1, W), S = A.scales(2, blocks(W.rows), blocks(W.cols));
   A.want_bytes(0, 2);
   void* s = A.stream(3);
@@ -368,6 +380,7 @@ NATIVE(fp8_quantize_weight) {
 // (Wq, WS, X, bias, act, Y, ws, stream)
 NATIVE(linear_fp8) {
   NATIVE_ARGS(linear_fp8, 8);
+  A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(5);
   A.want_bytes(0, 1);
   A.want_bytes(2, 2);
@@ -389,6 +402,7 @@ NATIVE(linear_fp8) {
 // (Wq, WS, Xq, XS, fmt, bias, act, Y, stream)
 NATIVE(linear_fp8_quantized) {
   NATIVE_ARGS(linear_fp8_quantized, 9);
+  A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(7);
   const Matrix XS = A.scales(3, X.rows, blocks(X.cols));
   A.want_bytes(0, 1);
@@ -410,6 +424,7 @@ NATIVE(linear_fp8_quantized) {
 // (Wq, WS, dYq, dYS, fmt, dX, stream)
 NATIVE(linear_fp8_backward_input) {
   NATIVE_ARGS(linear_fp8_backward_input, 7);
+  A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), dY = A.matrix(2), dX = A.matrix(5);
   const Matrix dYS = A.scales(3, dY.rows, blocks(dY.cols));
   A.want_bytes(0, 1);
@@ -429,6 +444,7 @@ NATIVE(linear_fp8_backward_input) {
 // (dYq, dYS, fmt_dy, Xq, XS, fmt_x, block, keep, dW, stream)
 NATIVE(linear_fp8_backward_weight) {
   NATIVE_ARGS(linear_fp8_backward_weight, 10);
+  A.one_device();
   const Matrix dY = A.matrix(0), dYS = A.scales(1, blocks(dY.rows), dY.cols), X = A.matrix(3), XS = A.scales(4, blocks(X.rows), X.cols);
   const Matrix dW = A.matrix(8);
   A.want_bytes(0, 1);
@@ -450,6 +466,7 @@ NATIVE(linear_fp8_backward_weight) {
 // (address of the job array, number of jobs, beta1, beta2, eps, step, seed, grad_scale, step_dev, stream)
 NATIVE(masked_adam_step_batched) {
   NATIVE_ARGS(masked_adam_step_batched, 10);
+  A.one_device();
   const bsp_adam_job* jobs = static_cast<const bsp_adam_job*>(A.address(0));
   const int n = A.i32(1), step = A.i32(5);
   const float b1 = A.f32(2), b2 = A.f32(3), eps = A.f32(4);

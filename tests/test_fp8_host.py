@@ -65,6 +65,32 @@ def test_quantize_refuses(change, status):
     assert quantize(**change) == status
 
 
+MOST = 0x7FFFFE00                                                  # largest size
+
+
+def test_sizes_beyond_the_kernels_counting():
+    big = MOST + 1
+    assert quantize(cols=big, ldx=big, ldq=big, lds=1 << 26) == UNSUPPORTED
+    assert bsp.lib.bsp_fp8_quantize_weight(P, 1, big, big, P, big, P, 1 << 26, None) == UNSUPPORTED
+    n = ctypes.c_size_t()
+    assert bsp.lib.bsp_linear_fp8_ws_bytes(1, big, ctypes.byref(n)) == UNSUPPORTED and bsp.lib.bsp_linear_fp8_ws_bytes(big, 1, ctypes.byref(n)) == UNSUPPORTED
+    f = bsp.lib.bsp_linear_fp8_quantized
+    for n_out, k, t in ((big, 16, 1), (16, big, 1), (16, 16, big)):
+        assert f(P, k, P, 1 << 26, n_out, k, P, k, P, 1 << 26, 0, t, None, 0, P, n_out, None) == UNSUPPORTED
+        assert bsp.lib.bsp_linear_fp8_backward_input(P, k, P, 1 << 26, n_out, k, P, n_out, P, 1 << 26, 0, t, P, k, None) == UNSUPPORTED
+        assert bsp.lib.bsp_linear_fp8_backward_weight(P, n_out, P, n_out, 0, P, k, P, k, 0, t, n_out, k, 1, None, P, k, None) == UNSUPPORTED
+    assert adam(adam_job(rows=1, cols=big, ldw=big, ldg=big, ldm=big)) == UNSUPPORTED
+
+
+def test_binding_refuses_what_is_not_on_a_device():
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    q, s = torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(4, 1, dtype=torch.uint8)
+    with pytest.raises((ValueError, RuntimeError)):
+        bsp.bsp_fp8_quantize(x, bsp.FP8_E4M3, q, s)
+    with pytest.raises(ValueError):
+        bsp.make_adam_job_array([bsp.AdamJob(W=x.float(), grad=x, m=x.float(), v=x.float(), lr=1.0)])
+
+
 def test_quantize_weight_refuses():
     f = bsp.lib.bsp_fp8_quantize_weight
     assert f(None, 128, 128, 128, P, 128, P, 1, None) == ARG and f(P, 128, 128, 128, P, 128, None, 1, None) == ARG

@@ -279,3 +279,127 @@ def test_scales_of_any_size():
     layer.forward(bsp.ACT_NONE)
     layer.backward_input()
     layer.backward_weight(False)
+
+
+def test_binding_refuses_other_shapes_and_types():
+    layer = Layer(9, 40, 200, 1)
+    X, Y = widened(layer.x_bits, 200), torch.zeros((9, 40), dtype=torch.int16, device=DEV)
+    ws = torch.empty(bsp.bsp_linear_fp8_ws_bytes(9, 200), dtype=torch.uint8, device=DEV)
+    call = lambda **c: bsp.bsp_linear_fp8(**{**dict(Wq=layer.Wq, WS=layer.WS, X=X, bias=None, act=0, Y=Y, ws=ws), **c})  # noqa: E731
+    call()
+    for c in (dict(X=X[:, :199]), dict(Y=Y[:8]), dict(Y=Y.float()), dict(WS=layer.WS[:, :1]), dict(X=X.float()), dict(bias=torch.zeros(39, dtype=torch.int16, device=DEV)),
+              dict(Wq=layer.Wq.to(torch.int16))):
+        with pytest.raises(ValueError):
+            call(**c)
+    with pytest.raises(bsp.BspError) as e:
+        call(ws=ws[:100])
+    assert e.value.status == -3
+    with pytest.raises(ValueError):
+        bsp.bsp_fp8_quantize(X, 0, torch.zeros((9, 200), dtype=torch.uint8, device=DEV), torch.zeros((9, 1), dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("t", [5, 300])
+def test_captured_and_on_another_stream(t):
+    """The calls of a training step, captured on one stream and replayed on new inputs while another stream runs the same step with its own
+    buffers: both get what single calls give."""
+    n, k, block = 264, 400, 8
+    layer = Layer(t, n, k, 17, block=block)
+    keep = torch.from_numpy(layer.keep).to(DEV)
+    inputs = [(widened(Layer(t, n, k, s, block=block).x_bits, k), widened(Layer(t, n, k, s, block=block).dy_bits, n)) for s in (21, 22, 23)]
+
+    def buffers():
+        u8 = lambda r, c: torch.zeros((r, up(c, 16)), dtype=torch.uint8, device=DEV)[:, :c]  # noqa: E731
+        i16 = lambda r, c: torch.zeros((r, c), dtype=torch.int16, device=DEV)  # noqa: E731
+        b = up(t, 128) // 128
+        return dict(xr=u8(t, k), xc=u8(t, k), yr=u8(t, n), yc=u8(t, n), xrs=u8(t, up(k, 128) // 128), xcs=u8(b, k), yrs=u8(t, up(n, 128) // 128), ycs=u8(b, n),
+                    X=i16(t, k), dY=i16(t, n), Y=i16(t, n), dX=i16(t, k), dW=i16(n, k), db=torch.zeros(n, dtype=torch.float32, device=DEV),
+                    ws=torch.empty(b * n * 4, dtype=torch.uint8, device=DEV))
+
+    def step(b):
+        bsp.bsp_fp8_quantize(b["X"], F.E4M3, b["xr"], b["xrs"], b["xc"], b["xcs"])
+        bsp.bsp_linear_fp8_quantized(layer.Wq, layer.WS, b["xr"], b["xrs"], F.E4M3, None, bsp.ACT_NONE, b["Y"])
+        bsp.bsp_fp8_quantize(b["dY"], F.E5M2, b["yr"], b["yrs"], b["yc"], b["ycs"], b["db"], b["ws"])
+        bsp.bsp_linear_fp8_backward_input(layer.Wq, layer.WS, b["yr"], b["yrs"], F.E5M2, b["dX"])
+        bsp.bsp_linear_fp8_backward_weight(b["yc"], b["ycs"], F.E5M2, b["xc"], b["xcs"], F.E4M3, block, keep, b["dW"])
+        return b
+
+    def fill(b, i):
+        b["X"].copy_(inputs[i][0])
+        b["dY"].copy_(inputs[i][1])
+        return b
+
+    names = ("Y", "dX", "dW", "db")
+    want = []
+    for i in range(3):
+        b = step(fill(buffers(), i))
+        torch.cuda.synchronize()
+        want.append({k: b[k].clone() for k in names})
+    a, c = buffers(), buffers()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a)
+    side = torch.cuda.Stream()
+    for i in range(3):
+        fill(a, i)
+        fill(c, 2 - i)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(3):
+                step(c)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in names:
+            assert torch.equal(a[k], want[i][k]), k
+            assert torch.equal(c[k], want[2 - i][k]), k
+    bsp.bsp_linear_status()
+    graph.reset()
+
+
+@pytest.mark.parametrize("block,t", [(16, 200), (1, 33)])
+def test_retraining_in_8_bits(block, t):
+    """The operators as a retraining loop uses them: prune, quantise the masked weight, forward and backward in 8 bits, the weight gradient
+    and bias gradient into one Adam step with 8-bit moments, whose bf16 copy is quantised for the next forward.  Two iterations; every piece against the oracle."""
+    n, k = 96, 200
+    rng = np.random.default_rng(block)
+    w = 0.02 * rng.normal(size=(n, k))
+    keep_np = (rng.random((n // block, k)) < 0.4).astype(np.uint8)
+    keep_np[0] = 0
+    mask = np.repeat(keep_np, block, 0).astype(bool)
+    W = torch.from_numpy((w * mask).astype(np.float32)).to(DEV)
+    b = torch.zeros((1, n), dtype=torch.float32, device=DEV)
+    Wb, bb = torch.zeros((n, k), dtype=torch.int16, device=DEV), torch.zeros((1, n), dtype=torch.int16, device=DEV)
+    keep = torch.from_numpy(keep_np).to(DEV)
+    state = lambda r, c: dict(m=torch.zeros((r, c), dtype=torch.uint8, device=DEV), v=torch.zeros((r, c), dtype=torch.uint8, device=DEV),  # noqa: E731
+                              m_scale=torch.zeros((r, up(c, 128) // 128), dtype=torch.uint8, device=DEV), v_scale=torch.zeros((r, up(c, 128) // 128), dtype=torch.uint8, device=DEV))
+    dW, db = torch.zeros((n, k), dtype=torch.int16, device=DEV), torch.zeros((1, n), dtype=torch.float32, device=DEV)
+    jobs = bsp.make_adam_job_array([bsp.AdamJob(W=W, grad=dW, lr=1e-3, weight_decay=0.01, keep=keep, block=block, W_bf16=Wb, **state(n, k)),
+                                    bsp.AdamJob(W=b, grad=db, lr=1e-3, W_bf16=bb, **state(1, n))])
+    Wb.copy_(torch.from_numpy(bf16_bits(w * mask).view(np.int16)))
+    kb, nb, tb = up(k, 128) // 128, up(n, 128) // 128, up(t, 128) // 128
+    u8 = lambda r, c: torch.zeros((r, up(c, 16)), dtype=torch.uint8, device=DEV)[:, :c]  # noqa: E731
+    Wq, WS = u8(n, k), u8(nb, kb)
+    xr, xc, yr, yc, xrs, xcs, yrs, ycs = u8(t, k), u8(t, k), u8(t, n), u8(t, n), u8(t, kb), u8(tb, k), u8(t, nb), u8(tb, n)
+    ws = torch.empty(tb * n * 4, dtype=torch.uint8, device=DEV)
+    Y, dX = torch.zeros((t, n), dtype=torch.int16, device=DEV), torch.zeros((t, k), dtype=torch.int16, device=DEV)
+    for step in (1, 2):
+        w_bits, b_bits = bits_of(Wb), bits_of(bb)[0]
+        x_bits, dy_bits = random_matrix(rng, t, k, 1.0), random_matrix(rng, t, n, 1.0)
+        bsp.bsp_fp8_quantize_weight(Wb, Wq, WS)
+        bsp.bsp_fp8_quantize(to_dev(x_bits), F.E4M3, xr, xrs, xc, xcs)
+        bsp.bsp_linear_fp8_quantized(Wq, WS, xr, xrs, F.E4M3, bb[0], bsp.ACT_NONE, Y)
+        bsp.bsp_fp8_quantize(to_dev(dy_bits), F.E5M2, yr, yrs, yc, ycs, db[0], ws)
+        bsp.bsp_linear_fp8_backward_input(Wq, WS, yr, yrs, F.E5M2, dX)
+        bsp.bsp_linear_fp8_backward_weight(yc, ycs, F.E5M2, xc, xcs, F.E4M3, block, keep, dW)
+        before = W.cpu().numpy()
+        bsp.bsp_masked_adam_step_batched(jobs, 0.9, 0.999, 1e-8, step, 7)
+        bsp.bsp_linear_status()
+        form = lambda bits, rows, cols, fmt: F.dequantize(*F.quantize(bf16_bits_to_f64(bits), rows, cols, fmt), rows, cols, fmt)  # noqa: E731
+        w8 = form(w_bits, 128, 128, F.E4M3)
+        check(bits_of(Y), form(x_bits, 1, 128, F.E4M3), w8, bf16_bits_to_f64(b_bits), what="Y")
+        check(bits_of(dX), form(dy_bits, 1, 128, F.E5M2), w8.T, what="dX")
+        check(bits_of(dW), form(dy_bits, 128, 1, F.E5M2).T, form(x_bits, 128, 1, F.E4M3).T, mask=mask, what="dW")
+        dy = bf16_bits_to_f64(dy_bits)
+        assert (np.abs(db[0].cpu().numpy() - dy.sum(0)) <= t * 2.0 ** -24 * np.abs(dy).sum(0)).all()
+        after = W.cpu().numpy()
+        assert not after[~mask].any() and (np.abs(after - before)[mask] > 0).mean() > 0.9
+        assert np.array_equal(bits_of(Wb), bf16_bits(after)) and b.abs().sum() > 0
