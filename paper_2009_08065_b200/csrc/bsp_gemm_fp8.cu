@@ -437,37 +437,48 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     uint32_t phase = 0, slot_phase = 0, scale_buf = 0, acc_phases = 0;
     int acc = 0;
     bool ok = true;
+    // The scales of the four blocks from kb on, to the set of columns that the four blocks before do not read; two stages ahead of the
+    // instructions that read them, which would otherwise wait for the copy.
+    auto bring_scales = [&](bool first_tile, int kb) {
+      const int group = ((kb >> 2) + (first_tile ? kSlotGroups - 1 : 0)) & (kSlotGroups - 1);      // (the first turn is one group)
+      if (group == 0 || kb == 0) {
+        if (!mbar_wait_warp(scale_full_bar(slot), slot_phase, P.status)) return false;
+        tcgen05_fence_after();
+      }
+      const uint32_t src = smem_base + kScalesOff + (slot * kSlotGroups + group) * kPairScaleGroup;
+      scale_buf ^= kPairScaleCols;
+      const uint32_t dst = tmem_base + 512u - 2u * kPairScaleCols + scale_buf;
+      for (int i = 0; i <= tiles_b; ++i) copy_scales_pair(dst + 4u * i, src + i * kScaleTile);
+      if (group == kSlotGroups - 1 || kb + 4 >= k_blocks) {
+        commit_both(scale_empty_bar(slot));
+        if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+      }
+      return true;
+    };
     begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
+      ok = bring_scales(tile == pair, 0);
+      if (!ok) break;
       if (!mbar_wait_warp(acc_empty_bar(acc), ((acc_phases >> acc) & 1u) ^ 1u, P.status)) { ok = false; break; }
       tcgen05_fence_after();
       const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * w);
       uint32_t sfa = 0u;
+      bool ready = false;
       for (int kb = 0; kb < k_blocks; ++kb) {
-        if ((kb & 3) == 0) {
-          // the next four blocks' scales (two sets of columns in turn: the instructions before still read the other one)
-          const int group = ((kb >> 2) + (tile == pair ? kSlotGroups - 1 : 0)) & (kSlotGroups - 1);      // (the first turn is one group)
-          if (group == 0 || kb == 0) {
-            if (!mbar_wait_warp(scale_full_bar(slot), slot_phase, P.status)) { ok = false; break; }
-            tcgen05_fence_after();
-          }
-          const uint32_t src = smem_base + kScalesOff + (slot * kSlotGroups + group) * kPairScaleGroup;
-          sfa = tmem_base + 512u - 2u * kPairScaleCols + scale_buf * kPairScaleCols;
-          scale_buf ^= 1u;
-          for (int i = 0; i <= tiles_b; ++i) copy_scales_pair(sfa + 4u * i, src + i * kScaleTile);
-          if (group == kSlotGroups - 1 || kb + 4 >= k_blocks) {
-            commit_both(scale_empty_bar(slot));
-            if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
-          }
-        }
-        if (!mbar_wait_warp(full_bar(stage), phase, P.status)) { ok = false; break; }
+        if ((kb & 3) == 0) sfa = tmem_base + 512u - 2u * kPairScaleCols + scale_buf;
+        if (!mbar_wait_probed(ready, full_bar(stage), phase, P.status)) { ok = false; break; }
         tcgen05_fence_after();
+        const int next = stage + 1 == S ? 0 : stage + 1;
+        const uint32_t next_phase = next ? phase : phase ^ 1u;
+        ready = kb + 1 < k_blocks && mbar_try_wait(full_bar(next), next_phase);
         const uint32_t a_addr = smem_base + stage * kPairStage, b_addr = a_addr + kBlockM * kBlock;
         const uint32_t idesc = P.idesc | (static_cast<uint32_t>(kb & 3) << 29) | (static_cast<uint32_t>(kb & 3) << 4);
         mma_stage_scaled_pair<kAMn ? 256 : 2, kBMn ? 256 : 2>(d_tmem, kAMn ? smem_desc_mn8(a_addr) : smem_desc_sw128(a_addr),
                                                               kBMn ? smem_desc_mn8(b_addr) : smem_desc_sw128(b_addr), idesc, kb != 0 ? 1u : 0u,
                                                               empty_bar(stage), sfa, sfa + 4u);
-        if (++stage == S) { stage = 0; phase ^= 1u; }
+        stage = next;
+        phase = next_phase;
+        if ((kb & 3) == 1 && kb + 3 < k_blocks && !bring_scales(tile == pair, kb + 3)) { ok = false; break; }
       }
       if (!ok) break;
       commit_both(acc_full_bar(acc));
