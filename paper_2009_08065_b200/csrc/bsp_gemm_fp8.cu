@@ -606,23 +606,34 @@ int launch_pair(const Product& p, int w, TcDevice* dev, cudaStream_t s) {
   return BSP_OK;
 }
 
-// Width of the tiles by their estimated time: waves of tiles, each with the stages' time (measured: from 0.25 us for 64 columns, where the
-// issue of a stage binds, to 0.43 us for 256) or the epilogue's where that is longer; a tile of 256 columns, with its one accumulator, has its
-// epilogue behind its stages.
+// Width of the tiles by their estimated time: waves of tiles, each with its stages' time and what the stores of the tile before keep of it, or
+// with GELU the epilogue's where that is longer; a tile of 256 columns, with its one accumulator, has its epilogue behind its
+// stages.  Microseconds of a stage measured on layers of 480 to 4096 features: a call alone, and in one of 30 us and more, where the
+// power limit takes a quarter of the clock.  Weights that lie the other way round, and column forms, are copied in whole boxes of 128 columns however
+// many are used, and from anything but multiples of 64 bytes slower: fewer widths.  Measured / best width: 4096 x 4096 x 1024 18.3 / 17.9 us (with GELU 22.3 / 22.3),
+// 4096 x 1024 x 4096 15.7 / 15.7, 16384 x 1024 x 4096 59.2 / 58.8, 1003 x 2128 x 928 6.4 / 6.4, 1024 x 1024 x 4096 9.4 / 9.4.
 int choose_width(const Product& p, int sms) {
-  struct Width { int w; double stage; };
-  constexpr Width kWidths[] = {{64, 0.255}, {128, 0.28}, {192, 0.325}, {240, 0.388}, {256, 0.43}};
+  struct Width { int w; double alone, among; };
+  constexpr Width kKMajor[] = {{64, 0.165, 0.194}, {96, 0.166, 0.21}, {128, 0.1875, 0.256}, {160, 0.20, 0.257}, {192, 0.23, 0.293}, {240, 0.28, 0.35}, {256, 0.33, 0.42}};
+  constexpr Width kMnMajor[] = {{64, 0.22, 0.26}, {128, 0.23, 0.27}, {192, 0.24, 0.30}, {256, 0.33, 0.42}};
+  const Width* widths = p.B.mn ? kMnMajor : kKMajor;
+  const int count = p.B.mn ? sizeof(kMnMajor) / sizeof(Width) : sizeof(kKMajor) / sizeof(Width);
   const int k_blocks = blocks_of(p.contraction);
+  const bool gelu = p.act == BSP_ACT_GELU;
   int best = 0;
-  double least = 0.0;
-  for (const Width& c : kWidths) {
-    if (p.B.mn && c.w % 32 != 0) continue;              // (half a tile's columns begin at a multiple of 16 bytes)
-    const long long tiles = static_cast<long long>((p.A.rows - 1) / 256 + 1) * ((p.B.rows - 1) / c.w + 1);
-    const long long waves = (tiles + sms / 2 - 1) / (sms / 2);
-    const double stages = k_blocks * c.stage * (p.A.mn ? 1.1 : 1.0), epilogue = c.w * (p.act == BSP_ACT_GELU ? 0.013 : 0.006);
-    const double wave = pair_accumulators(c.w) == 2 ? fmax(stages, epilogue) : stages + epilogue;
-    const double t = (waves - 1) * wave + stages + epilogue;
-    if (best == 0 || t < least) { best = c.w; least = t; }
+  for (const bool among : {false, true}) {
+    double least = 0.0;
+    best = 0;
+    for (int i = 0; i < count; ++i) {
+      const int w = widths[i].w;
+      const long long tiles = static_cast<long long>((p.A.rows - 1) / 256 + 1) * ((p.B.rows - 1) / w + 1);
+      const long long waves = (tiles + sms / 2 - 1) / (sms / 2);
+      const double stages = k_blocks * (among ? widths[i].among : widths[i].alone), last = w * (gelu ? 0.0125 : 0.0075);
+      const double wave = pair_accumulators(w) == 1 ? stages + w * (gelu ? 0.011 : 0.007) : gelu ? fmax(stages + 0.004 * w, 0.6 + 0.0152 * w) : stages + 0.004 * w;
+      const double t = (waves - 1) * wave + stages + last;
+      if (best == 0 || t < least) { best = w; least = t; }
+    }
+    if (least < 30.0) break;
   }
   return best;
 }
