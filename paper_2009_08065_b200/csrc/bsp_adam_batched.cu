@@ -108,20 +108,20 @@ __device__ __forceinline__ float one_if_less(float a, float b) {
 // Two magnitudes (not negative, in the format's range) to one of their two neighbours in the format: random bits are added at the
 // upper end of what is then cut off (r: 16 of them).  Below the smallest normal value steps are as wide as just above it, so that
 // value is added first and taken off again.  (The integer pipe, at half the rate of the others, is what this kernel fills:
-// hence a comparison that gives 1 or 0 as float32, and a multiply-add for the random bits.)
+// hence a comparison that gives 1 or 0 as float32, and a multiply-add for the random bits.  The two values go one by one here: packed
+// operations between single ones cost more moves than they save, 302 M weights 947 us and 937.)
 template <int FMT>
 __device__ __forceinline__ Pair round_pair(Pair y, uint32_t r0, uint32_t r1) {
   constexpr int kDrop = FMT == BSP_FP8_E4M3 ? 20 : 21;
   constexpr uint32_t kKeep = ~((1u << kDrop) - 1u);
   constexpr float kLow = FMT == BSP_FP8_E4M3 ? 0x1p-6f : 0x1p-14f;
-  float y0, y1, z0, z1;
+  float y0, y1;
   split(y, y0, y1);
-  const Pair below = pair_of(one_if_less(y0, kLow), one_if_less(y1, kLow));
-  split(fma(below, pair_of(kLow), y), z0, z1);
+  const float b0 = one_if_less(y0, kLow), b1 = one_if_less(y1, kLow);
   uint32_t u0, u1;
-  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u0) : "r"(r0), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(z0)));
-  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u1) : "r"(r1), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(z1)));
-  return fma(below, pair_of(-kLow), pair_of(__uint_as_float(u0 & kKeep), __uint_as_float(u1 & kKeep)));
+  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u0) : "r"(r0), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(__fmaf_rn(b0, kLow, y0))));
+  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(u1) : "r"(r1), "n"(1 << (kDrop - 16)), "r"(__float_as_uint(__fmaf_rn(b1, kLow, y1))));
+  return pair_of(__fmaf_rn(b0, -kLow, __uint_as_float(u0 & kKeep)), __fmaf_rn(b1, -kLow, __uint_as_float(u1 & kKeep)));
 }
 // Denormal values count as zero.
 __device__ __forceinline__ float square_root(float x) {
@@ -289,9 +289,10 @@ adam_batched_kernel(const __grid_constant__ AdamTable T) {
   store_weights(J, p, w);
 }
 
-// 8-bit moments.  HBM allows 90 issue slots (45 of the integer pipe) for a warp's 32 weights, and the arithmetic needs most of them, hence
-// packed float32 operations, and the hardware's approximate square root and reciprocal (each within about a place) for the update of W
-// (the moments, which the 8-bit values follow to the last bit, are rounded as defined).
+// 8-bit moments.  HBM allows 90 issue slots (45 of the integer pipe) for a warp's 32 weights, and the kernel takes 84 (35), of which the random
+// bits are 11: it runs 1.25 times as long as its bytes would (without the hash 889 us in place of 947).  Hence packed float32 operations, and
+// the hardware's approximate square root and reciprocal (each within about a place) for the update of W (the moments, which the 8-bit
+// values follow to the last bit, are rounded as defined).
 // Eight weights as they lie in memory.
 struct Raw {
   uint4 w[2], g[2];            // g: float32, or bf16 in the first half
@@ -354,7 +355,8 @@ __device__ __forceinline__ Stepped step_eight(const Raw& x, uint32_t position, c
   out.byte_m = bad_m ? 127 : scale_byte(top_m, top_of(BSP_FP8_E4M3));
   out.byte_v = bad_v ? 127 : scale_byte(top_v, top_of(BSP_FP8_E5M2));
   const Pair inv_m = pair_of(scale_inverse(out.byte_m)), inv_v = pair_of(scale_inverse(out.byte_v));
-  uint32_t out_m[4], out_v[4];
+  uint32_t out_m[2], out_v[2];
+  float qm[8], qv[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t m_bits[2], v_bits[2];
@@ -367,16 +369,20 @@ __device__ __forceinline__ Stepped step_eight(const Raw& x, uint32_t position, c
     float lo, hi, a, b;
     split(m[i], a, b);
     split(round_pair<BSP_FP8_E4M3>(mul(pair_of(fabsf(a), fabsf(b)), inv_m), m_bits[0], m_bits[1]), lo, hi);
-    out_m[i] = to_fp8x2<BSP_FP8_E4M3>(copysignf(lo, a), copysignf(hi, b));
+    qm[2 * i] = copysignf(lo, a);
+    qm[2 * i + 1] = copysignf(hi, b);
+    if (i & 1) out_m[i >> 1] = to_fp8x4<BSP_FP8_E4M3>(qm[2 * i - 2], qm[2 * i - 1], qm[2 * i], qm[2 * i + 1]);
     // A positive value below the smallest one becomes that, which random bits leave as it is.
     split(v[i], lo, hi);
     split(mul(pair_of(one_if_less(0.0f, lo), one_if_less(0.0f, hi)), pair_of(0x1p-16f)), a, b);
     split(mul(v[i], inv_v), lo, hi);
     split(round_pair<BSP_FP8_E5M2>(pair_of(fmaxf(lo, a), fmaxf(hi, b)), v_bits[0], v_bits[1]), lo, hi);
-    out_v[i] = to_fp8x2<BSP_FP8_E5M2>(lo, hi);
+    qv[2 * i] = lo;
+    qv[2 * i + 1] = hi;
+    if (i & 1) out_v[i >> 1] = to_fp8x4<BSP_FP8_E5M2>(qv[2 * i - 2], qv[2 * i - 1], qv[2 * i], qv[2 * i + 1]);
   }
-  out.m = make_uint2(out_m[0] | (out_m[1] << 16), out_m[2] | (out_m[3] << 16));
-  out.v = make_uint2(out_v[0] | (out_v[1] << 16), out_v[2] | (out_v[3] << 16));
+  out.m = make_uint2(out_m[0], out_m[1]);
+  out.v = make_uint2(out_v[0], out_v[1]);
   if (bad_m) out.m = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
   if (bad_v) out.v = make_uint2(kNan * 0x01010101u, kNan * 0x01010101u);
   return out;
@@ -392,10 +398,10 @@ __device__ __forceinline__ void rates(const AdamTable& T, const AdamJob& J, Rate
 }
 
 // Tensors without gaps whose rows are whole pieces of eight, masked along columns or not at all.  Sixteen blocks of 128 lie next to each
-// other in memory then, and reach shared memory by bulk copies, two such chunks ahead: 100 KB on their way per SM.  (A fourth stage takes its room from L1, where the flags of a block's
-// rows are found again: 302 M weights 1006 us with three stages, 1054 with four.)  Loads to registers,
-// also one turn ahead, came to half of that at 24 warps per SM, and the kernel waited for them: 302 M weights 1088 us and more however little was
-// computed.  CTAs that run at once work on neighbouring chunks.
+// other in memory then, and reach shared memory by bulk copies, two such chunks ahead: 100 KB on their way per SM.  Loads to registers, also one
+// turn ahead, came to half of that at 24 warps per SM, and the kernel waited for them: 302 M weights 1088 us however little was computed, this
+// way 937 (5.2 TB/s).  A fourth stage takes its room from L1, where the flags of a block's rows are found again (5 % slower); four and five CTAs per
+// SM, with fewer registers, were no faster.  CTAs that run at once work on neighbouring chunks.
 constexpr int kChunk = kAdamGroups * kBlock;       // weights
 constexpr int kStreamCtas = 3;                     // of an SM
 constexpr int kStreamStages = 3;

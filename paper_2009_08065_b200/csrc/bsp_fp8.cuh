@@ -41,20 +41,25 @@ __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_f
 __device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float(static_cast<uint32_t>(254 - byte) << 23); }
 __host__ __device__ constexpr int top_of(int fmt) { return fmt == BSP_FP8_E4M3 ? 8 : 15; }
 
-// Two values, lo in the lower byte.
-template <int FMT>
-__device__ __forceinline__ uint32_t to_fp8x2(float lo, float hi) {
-  uint16_t r;
-  if (FMT == BSP_FP8_E4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
+// The two values of the lower half, the first in the lower byte.
 template <int FMT>
 __device__ __forceinline__ void from_fp8x2(uint32_t two, float& lo, float& hi) {
   uint32_t h;
   if (FMT == BSP_FP8_E4M3) asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
   else asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
   asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
+}
+// Four values, the first in the lowest byte.
+template <int FMT>
+__device__ __forceinline__ uint32_t to_fp8x4(float x0, float x1, float x2, float x3) {
+  uint32_t r;
+  if (FMT == BSP_FP8_E4M3)
+    asm("{\n\t.reg .b16 l, u;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 u, %4, %3;\n\tmov.b32 %0, {l, u};\n\t}"
+        : "=r"(r) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+  else
+    asm("{\n\t.reg .b16 l, u;\n\tcvt.rn.satfinite.e5m2x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 u, %4, %3;\n\tmov.b32 %0, {l, u};\n\t}"
+        : "=r"(r) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+  return r;
 }
 // The larger magnitudes of two pairs of bf16 values, NaN where there is one (signs are left undefined).
 __device__ __forceinline__ uint32_t abs_max2(uint32_t a, uint32_t b) {
@@ -76,8 +81,8 @@ __device__ __forceinline__ uint32_t block_scale(uint32_t amax16, float& inv) {
 // Four values times their multipliers as 8 bits.
 template <int FMT>
 __device__ __forceinline__ uint32_t four_to_fp8(uint32_t x0, uint32_t x1, float i0, float i1, float i2, float i3) {
-  return to_fp8x2<FMT>(__uint_as_float(x0 << 16) * i0, __uint_as_float(x0 & 0xffff0000u) * i1) |
-         (to_fp8x2<FMT>(__uint_as_float(x1 << 16) * i2, __uint_as_float(x1 & 0xffff0000u) * i3) << 16);
+  return to_fp8x4<FMT>(__uint_as_float(x0 << 16) * i0, __uint_as_float(x0 & 0xffff0000u) * i1, __uint_as_float(x1 << 16) * i2,
+                       __uint_as_float(x1 & 0xffff0000u) * i3);
 }
 #endif
 

@@ -33,14 +33,18 @@ struct QuantArgs {
   int wide_in, wide_out;     // 16-byte loads; stores of 16 (2), 8 (1) or single bytes (0)
 };
 
-// A pair of values times a pair of multipliers, as 8 bits.
+// A pair of bf16 values as float32, and times a pair of multipliers.
+__device__ __forceinline__ unsigned long long values_of(uint32_t x) { return tc::pack_f32x2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+// Two pairs of values times their multipliers, as 8 bits.
 template <int FMT>
-__device__ __forceinline__ uint32_t pair_times(unsigned long long v, unsigned long long m) {
-  float lo, hi;
-  unsigned long long p;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p) : "l"(v), "l"(m));
-  tc::unpack_f32x2(p, lo, hi);
-  return to_fp8x2<FMT>(lo, hi);
+__device__ __forceinline__ uint32_t four_times(unsigned long long v0, unsigned long long v1, unsigned long long m0, unsigned long long m1) {
+  float x[4];
+  unsigned long long p0, p1;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p0) : "l"(v0), "l"(m0));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p1) : "l"(v1), "l"(m1));
+  tc::unpack_f32x2(p0, x[0], x[1]);
+  tc::unpack_f32x2(p1, x[2], x[3]);
+  return to_fp8x4<FMT>(x[0], x[1], x[2], x[3]);
 }
 __device__ __noinline__ void store_some(uint8_t* dst, uint4 q, int n) {
   unsigned long long v = q.x | (static_cast<unsigned long long>(q.y) << 32);
@@ -51,8 +55,9 @@ __device__ __noinline__ void store_some(uint8_t* dst, uint4 q, int n) {
   }
 }
 // Sixteen bytes, of which n exist.
+template <bool kWhole = false>
 __device__ __forceinline__ void store_sixteen(uint8_t* dst, const uint32_t (&q)[4], int n, int wide) {
-  if (wide == 2 && n == 16) {
+  if (kWhole || (wide == 2 && n == 16)) {
     *reinterpret_cast<uint4*>(dst) = make_uint4(q[0], q[1], q[2], q[3]);
   } else if (wide >= 1 && n >= 8 && (n & 7) == 0) {
     *reinterpret_cast<uint2*>(dst) = make_uint2(q[0], q[1]);
@@ -75,7 +80,7 @@ __device__ __noinline__ uint4 load_some(const uint16_t* src, int n) {
   return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32));
 }
 // A thread's rows x 16 columns of the tile, as pairs.
-template <int ROWS>
+template <bool kWhole, int ROWS>
 __device__ __forceinline__ void load_tile(const QuantArgs& A, int r0, int c, int n, uint32_t (&x)[ROWS][8]) {
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {           // evenly spread from this thread's first one on
@@ -84,8 +89,8 @@ __device__ __forceinline__ void load_tile(const QuantArgs& A, int r0, int c, int
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (r < A.rows) {
-        if (A.wide_in && n >= 8 * h + 8) {
+      if (kWhole || r < A.rows) {
+        if (kWhole || (A.wide_in && n >= 8 * h + 8)) {
           v = ld_global(reinterpret_cast<const uint4*>(src + 8 * h));
         } else if (n > 8 * h) {
           v = load_some(src + 8 * h, min(8, n - 8 * h));
@@ -116,7 +121,7 @@ quantize_kernel(QuantArgs A) {
   pdl_wait();
   pdl_launch_dependents();
   uint32_t x[4][8];
-  load_tile(A, r0, c, n, x);
+  load_tile<false>(A, r0, c, n, x);
   uint32_t tile = 0u;
   if (kTile) {
 #pragma unroll
@@ -144,12 +149,13 @@ quantize_kernel(QuantArgs A) {
   }
 }
 
-// Along the columns, and column sums and along the rows where they are asked for.  Bound by issue beside HBM (8 instructions a value):
-// every pair is unpacked once for both forms and multiplied as a pair.  4096 x 4096 15.6 us (10.3 of HBM), with column sums 17.5; 512 threads with
-// two rows each were no faster.
-template <int FMT>
-__global__ void __launch_bounds__(kQuantThreads, 4)
-quantize_both_kernel(QuantArgs A) {
+// Along the columns, and column sums and along the rows where they are asked for.  Bound by issue beside HBM (14 instructions a value,
+// 18 with column sums, and half of the time waiting for the other warps' maxima): every pair is unpacked once for both forms and multiplied
+// as a pair, and whole tiles have a body without conditions.  4096 x 4096 14.7 us (10.3 of HBM; 15.7 with one body for all tiles), with column sums
+// 17.3; 512 threads with two rows each, or the rows' form ahead of the barrier, were no faster.
+// kWhole: the tile is whole, and its rows begin at multiples of 16 bytes everywhere.
+template <int FMT, bool kWhole>
+__device__ __forceinline__ void quantize_both(const QuantArgs& A) {
   constexpr int kRows = kBlock * 8 / kQuantThreads, kWarps = kQuantThreads / 32, kStep = kBlock / kRows;
   __shared__ uint32_t s_max[kWarps][64];     // [warp][pair of columns]
   __shared__ __align__(16) float s_inv[128];
@@ -157,10 +163,8 @@ quantize_both_kernel(QuantArgs A) {
   const int warp = threadIdx.x >> 5, l = threadIdx.x & 7, slot = threadIdx.x >> 3;
   const int r0 = blockIdx.y * kBlock + slot, c0 = blockIdx.x * kBlock, c = c0 + 16 * l;
   const int n = max(0, min(16, A.cols - c));
-  pdl_wait();
-  pdl_launch_dependents();
   uint32_t x[kRows][8];
-  load_tile(A, r0, c, n, x);
+  load_tile<kWhole>(A, r0, c, n, x);
   if (A.q_col != nullptr) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -201,7 +205,7 @@ quantize_both_kernel(QuantArgs A) {
         float inv;
         const uint32_t byte = block_scale<FMT>((u ? m >> 16 : m) & 0x7fffu, inv);
         s_inv[at] = inv;
-        if (c0 + at < A.cols) A.s_col[static_cast<size_t>(blockIdx.y) * A.lds_col + c0 + at] = static_cast<uint8_t>(byte);
+        if (kWhole || c0 + at < A.cols) A.s_col[static_cast<size_t>(blockIdx.y) * A.lds_col + c0 + at] = static_cast<uint8_t>(byte);
       }
     }
   } else if (A.partial != nullptr && threadIdx.x >= 128 && c0 + static_cast<int>(threadIdx.x) - 128 < A.cols) {
@@ -219,7 +223,7 @@ quantize_both_kernel(QuantArgs A) {
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     const int r = r0 + kStep * i;
-    if (r >= A.rows) continue;
+    if (!kWhole && r >= A.rows) continue;
     float inv = 0.0f;
     if (A.q_row != nullptr) {
       const uint32_t byte = block_scale<FMT>(top[i], inv);
@@ -229,15 +233,23 @@ quantize_both_kernel(QuantArgs A) {
     uint32_t q[4], p[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      const unsigned long long v0 = values_of(x[i][2 * j]), v1 = values_of(x[i][2 * j + 1]);
+      q[j] = four_times<FMT>(v0, v1, along, along);
       const float4 down = A.q_col != nullptr ? reinterpret_cast<const float4*>(s_inv)[4 * l + j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const unsigned long long v0 = tc::pack_f32x2(__uint_as_float(x[i][2 * j] << 16), __uint_as_float(x[i][2 * j] & 0xffff0000u));
-      const unsigned long long v1 = tc::pack_f32x2(__uint_as_float(x[i][2 * j + 1] << 16), __uint_as_float(x[i][2 * j + 1] & 0xffff0000u));
-      q[j] = pair_times<FMT>(v0, along) | (pair_times<FMT>(v1, along) << 16);
-      p[j] = pair_times<FMT>(v0, tc::pack_f32x2(down.x, down.y)) | (pair_times<FMT>(v1, tc::pack_f32x2(down.z, down.w)) << 16);
+      p[j] = four_times<FMT>(v0, v1, tc::pack_f32x2(down.x, down.y), tc::pack_f32x2(down.z, down.w));
     }
-    if (A.q_row != nullptr) store_sixteen(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
-    if (A.q_col != nullptr) store_sixteen(A.q_col + static_cast<size_t>(r) * A.ld_col + c, p, n, A.wide_out);
+    if (A.q_row != nullptr) store_sixteen<kWhole>(A.q_row + static_cast<size_t>(r) * A.ld_row + c, q, n, A.wide_out);
+    if (A.q_col != nullptr) store_sixteen<kWhole>(A.q_col + static_cast<size_t>(r) * A.ld_col + c, p, n, A.wide_out);
   }
+}
+template <int FMT>
+__global__ void __launch_bounds__(kQuantThreads, 4)
+quantize_both_kernel(QuantArgs A) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const bool whole = A.wide_in && A.wide_out == 2 && static_cast<int>(blockIdx.y + 1) * kBlock <= A.rows && static_cast<int>(blockIdx.x + 1) * kBlock <= A.cols;
+  if (whole) quantize_both<FMT, true>(A);
+  else quantize_both<FMT, false>(A);
 }
 
 // The blocks' column sums: four runs of blocks side by side, and the runs in their order.
