@@ -87,9 +87,9 @@ int check_weight(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out
 Operand weight_operand(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out) {
   return Operand{static_cast<const uint8_t*>(Wq), n_out, ldw, 0, BSP_FP8_E4M3, WS, ldws, 1, 7};
 }
-// Few tokens and a large weight: the CTAs of 16 outputs would each bring all tokens to 8 bits (13 tokens, 4096 x 4096: in one launch 10.8 us, quantised
-// first 9.4; 4096 x 1024: 3.6 and 4.4), and from some 16 tokens on the pairs are faster (32 tokens, 4096 x 4096: 18.6, 14.5, and 12.4 by pairs; 1024 x
-// 4096: 6.5, 6.8 and 11.8).
+// Few tokens and a large weight: the CTAs of 16 outputs would each bring all tokens to 8 bits.  In one launch / quantised first (us): 8 tokens, 4096 x
+// 4096 6.4 / 6.2, 13 tokens 9.5 / 9.2, 32 tokens 16 / 8.2; smaller weights, 4096 x 1024 with 13 tokens 3.5 / 4.4, 32 tokens 5.9 / 5.8, 1024 x 1024 with 32
+// tokens 4.2 / 4.8.
 bool large_weight(int n_out, int k_in) { return static_cast<long long>(n_out) * k_in >= (8ll << 20); }
 int row_pitch(int k_in) { return (k_in - 1) / 16 * 16 + 16; }
 

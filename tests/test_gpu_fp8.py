@@ -237,6 +237,34 @@ def test_backward_weight(t, n, k, block, fmt):
     layer.backward_weight(True)
 
 
+# Many output tiles (pairs of CTAs), few of them (clusters that share the contraction), contractions of one block to some 260, and whose
+# parts are more blocks than a CTA has stages or carries scales for at a time.
+LONG = [(1300, 1100, 1050, 10), (40, 96, 33000, 8), (100, 128, 30000, 16), (100, 30000, 128, 16), (9000, 96, 130, 8), (1000, 1000, 1200, 8),
+        (33, 1024, 1024, 8), (128, 768, 2300, 8), (200, 70, 5000, 10), (2300, 260, 200, 4)]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("t,n,k,block", LONG)
+def test_few_and_many_tiles(t, n, k, block, fmt):
+    layer = Layer(t, n, k, t + n + k, fmt, block=block)
+    layer.forward(bsp.ACT_GELU if k < 2000 else bsp.ACT_NONE)
+    layer.backward_input()
+    layer.backward_weight(True)
+
+
+def test_the_same_bits_every_time():
+    """Split contractions are added in a fixed order, whichever CTA is ready first."""
+    layer = Layer(130, 512, 4096, 3)
+    _, (Xq, XS) = layer.rows_form(layer.x_bits, layer.fmt)
+    runs = []
+    for _ in range(20):
+        Y = layer.out(130, 512)
+        bsp.bsp_linear_fp8_quantized(layer.Wq, layer.WS, Xq, XS, layer.fmt, None, bsp.ACT_NONE, Y.t)
+        runs.append(Y)
+    bsp.bsp_linear_status()
+    assert all(np.array_equal(r.host(), runs[0].host()) for r in runs)
+
+
 @pytest.mark.parametrize("t,n,k", [(1, 16, 128), (1, 1, 1), (1, 1000, 1000), (2, 130, 257), (7, 96, 100), (8, 64, 4096), (9, 200, 384), (15, 257, 1288), (16, 48, 130),
                                    (17, 40, 520), (31, 100, 136), (32, 256, 1024), (33, 128, 256), (64, 520, 768), (200, 130, 1000)])
 @pytest.mark.parametrize("pad", [0, 3])
