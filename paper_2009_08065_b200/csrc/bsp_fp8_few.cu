@@ -10,7 +10,7 @@
 // The legacy tensor instruction is enough here: 16 x 8 outputs a warp leave it idle most of the time, and tcgen05's 128-row tiles would need the
 // operands in shared memory first.
 // Times, the weight in L2: 1 token, 1024 -> 4096 with GELU 2.6 us; 13 tokens, 4096 -> 1024 4.2 us.  What bounds it is the chain of dependent steps: launch
-// and first loads, one block's arithmetic, the meeting of the sums.  Beyond a few tokens see large_weight (bsp_linear_fp8.cu).
+// and first loads, one block's arithmetic, the meeting of the sums.  Where it ends: few_is_faster (bsp_linear_fp8.cu).
 #include "bsp_fp8_gemm.cuh"
 #include "bsp_tc.cuh"
 
@@ -221,9 +221,10 @@ int launch_few_of(FewArgs A, cudaStream_t s) {
   while (ranks < 4 && tiles * ranks * 2 <= kFewCtas && blocks / (ranks * 2) >= kFewLeastBlocks) ranks *= 2;
   const int each = (blocks - 1) / ranks + 1, warps = each < kFewMaxWarps ? each : kFewMaxWarps;
   const int groups = tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4;
+  constexpr int kMostGroups = (kReady ? kFewReady : kFewTokens) / 8;
   auto kernel = groups == 1   ? linear_few_kernel<1, kReady, FMT>
                 : groups == 2 ? linear_few_kernel<2, kReady, FMT>
-                              : linear_few_kernel<4, kReady, FMT>;
+                              : linear_few_kernel<kMostGroups, kReady, FMT>;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles) * ranks);
   cfg.blockDim = dim3(32 * warps);

@@ -21,8 +21,8 @@ struct Product {
 bool tensor_core_ok(const Product& p);
 int launch_tensor_core(const Product& p, cudaStream_t s);
 
-// bsp_fp8_few.cu: the forward product for few tokens, from bf16 activations and from 8-bit ones (of any 16-byte aligned rows).
-constexpr int kFewTokens = 32;
+// bsp_fp8_few.cu: the forward product for few tokens, from up to 32 of bf16 and up to 16 of 8-bit ones (of any 16-byte aligned rows).
+constexpr int kFewTokens = 32, kFewReady = 16;
 bool few_tokens_ok(const void* Wq, int ldw, int tokens);
 int launch_few(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* X, int tokens, int ldx, const void* bias, int act,
                void* Y, int ldy, cudaStream_t s);

@@ -25,7 +25,8 @@ constexpr int kWarpEpi = 32 * kEpiCols * 2;        // an epilogue warp's 32 rows
 struct Fp8Params {
   Operand A, B;
   int contraction;
-  int b_bytes, width;        // bytes of one B copy, columns of a tile
+  int a_bytes, b_bytes;      // of one copy
+  int width;                 // columns of a tile
   uint32_t idesc;
   int act;
   const uint16_t* bias;      // [B.rows], or null
@@ -234,7 +235,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     const bool for_a = warp == 0;
     const CUtensorMap* map = for_a ? &map_a : &map_b;
     const uint32_t at = for_a ? 0u : static_cast<uint32_t>(kBlockM * kBlock);
-    const uint32_t arm = rank == 0 ? 2u * static_cast<uint32_t>(for_a ? kBlockM * kBlock : P.b_bytes) : 0u;      // both CTAs' bytes
+    const uint32_t arm = rank == 0 ? 2u * static_cast<uint32_t>(for_a ? P.a_bytes : P.b_bytes) : 0u;      // both CTAs' bytes
     const bool mn = for_a ? kAMn : kBMn;
     const uint32_t leader_full = map_to_cta(full_bar(0), 0);
     int stage = 0;
@@ -440,11 +441,11 @@ int launch_pair(const Product& p, int w, TcDevice* dev, cudaStream_t s) {
   static OncePerDevice once;
   BSP_TRY(allow_dynamic_smem(once, gemm_fp8_pair_kernel<kAMn, kBMn>, kPairSmem));
   CUtensorMap map_a, map_b;
-  const int b_rows = kBMn ? kBlock : w / 2;
-  if (!(kAMn ? make_map8(&map_a, p.A.q, p.A.rows, p.contraction, p.A.ld, kBlock) : make_map8(&map_a, p.A.q, p.contraction, p.A.rows, p.A.ld, kBlockM)) ||
+  const int a_rows = kAMn ? kBlock : box_rows(p.A.rows, kBlockM), b_rows = kBMn ? kBlock : box_rows(p.B.rows, w / 2);
+  if (!(kAMn ? make_map8(&map_a, p.A.q, p.A.rows, p.contraction, p.A.ld, kBlock) : make_map8(&map_a, p.A.q, p.contraction, p.A.rows, p.A.ld, a_rows)) ||
       !(kBMn ? make_map8(&map_b, p.B.q, p.B.rows, p.contraction, p.B.ld, kBlock) : make_map8(&map_b, p.B.q, p.contraction, p.B.rows, p.B.ld, b_rows)))
     return BSP_ERR_CUDA;
-  const Fp8Params P{p.A, p.B, p.contraction, b_rows * kBlock, w, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, 256, w), p.act, p.bias,
+  const Fp8Params P{p.A, p.B, p.contraction, a_rows * kBlock, b_rows * kBlock, w, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, 256, w), p.act, p.bias,
                     p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, dev->status};
   const long long tiles = static_cast<long long>((p.A.rows - 1) / 256 + 1) * ((p.B.rows - 1) / w + 1);
   const int pairs = tiles < dev->sms / 2 ? static_cast<int>(tiles) : dev->sms / 2;

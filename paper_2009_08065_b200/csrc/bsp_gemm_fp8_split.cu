@@ -28,6 +28,7 @@ static_assert(kTileN + 8 * kTurn / 4 * kMostTurns <= static_cast<int>(kTmemCols)
 struct Split8Params {
   Operand A, B;
   int n_tiles, k_blocks, stages;
+  int a_bytes, b_bytes;      // of one copy
   int recv_off, tail_off;    // offsets of the receive buffers and of scales, mbarriers and bias
   uint32_t idesc;
   int act;
@@ -107,11 +108,11 @@ gemm_fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
   ScalesB<kAMn> scales_b;
   auto load_a = [&](int i, int stage) {
     const int k = (kb0 + i) * kBlock;
-    tma_stage_load(smem_base + stage * kStage, &map_a, kAMn ? m0 : k, kAMn ? k : m0, full_bar(stage), kBlockM * kBlock);
+    tma_stage_load(smem_base + stage * kStage, &map_a, kAMn ? m0 : k, kAMn ? k : m0, full_bar(stage), P.a_bytes);
   };
   auto load_b = [&](int i, int stage) {
     const int k = (kb0 + i) * kBlock;
-    tma_stage_load(smem_base + stage * kStage + kBlockM * kBlock, &map_b, kBMn ? n0 : k, kBMn ? k : n0, full_bar(stage), stage_b(kBMn));
+    tma_stage_load(smem_base + stage * kStage + kBlockM * kBlock, &map_b, kBMn ? n0 : k, kBMn ? k : n0, full_bar(stage), P.b_bytes);
   };
   if (warp == 0) {
     // a lane for each barrier: all in one go
@@ -331,8 +332,9 @@ int launch_split8(const Product& p, TcDevice* dev, cudaStream_t s) {
   auto kernel = gemm_fp8_split_kernel<kAMn, kBMn, C>;
   BSP_TRY(allow_dynamic_smem(once, kernel, kSmemLimit));
   CUtensorMap map_a, map_b;
-  if (!(kAMn ? make_map8(&map_a, p.A.q, p.A.rows, p.contraction, p.A.ld, kBlock) : make_map8(&map_a, p.A.q, p.contraction, p.A.rows, p.A.ld, kBlockM)) ||
-      !(kBMn ? make_map8(&map_b, p.B.q, p.B.rows, p.contraction, p.B.ld, kBlock) : make_map8(&map_b, p.B.q, p.contraction, p.B.rows, p.B.ld, kTileN)))
+  const int a_rows = kAMn ? kBlock : box_rows(p.A.rows, kBlockM), b_rows = kBMn ? kBlock : box_rows(p.B.rows, kTileN);
+  if (!(kAMn ? make_map8(&map_a, p.A.q, p.A.rows, p.contraction, p.A.ld, kBlock) : make_map8(&map_a, p.A.q, p.contraction, p.A.rows, p.A.ld, a_rows)) ||
+      !(kBMn ? make_map8(&map_b, p.B.q, p.B.rows, p.contraction, p.B.ld, kBlock) : make_map8(&map_b, p.B.q, p.contraction, p.B.rows, p.B.ld, b_rows)))
     return BSP_ERR_CUDA;
   constexpr int kReceive = (C - 1) * kBlockM * (kTileN / C) * 4;
   constexpr int kFit = (kSmemLimit - 1024 - kTail - kReceive) / stage_bytes(kBMn) < kMostStages ? (kSmemLimit - 1024 - kTail - kReceive) / stage_bytes(kBMn)
@@ -342,7 +344,7 @@ int launch_split8(const Product& p, TcDevice* dev, cudaStream_t s) {
   const int recv_off = stages * stage_bytes(kBMn);
   int tail_off = recv_off + kReceive;
   if (tail_off < kSmemLimit / 2 + 1024) tail_off = kSmemLimit / 2 + 1024;                // one CTA per SM
-  const Split8Params P{p.A, p.B, n_tiles, k_blocks, stages, recv_off, tail_off, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, kBlockM, kTileN), p.act, p.bias,
+  const Split8Params P{p.A, p.B, n_tiles, k_blocks, stages, a_rows * kBlock, b_rows * kBlock, recv_off, tail_off, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, kBlockM, kTileN), p.act, p.bias,
                        p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, dev->status};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(((p.A.rows - 1) / kBlockM + 1) * n_tiles * C);

@@ -87,10 +87,15 @@ int check_weight(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out
 Operand weight_operand(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out) {
   return Operand{static_cast<const uint8_t*>(Wq), n_out, ldw, 0, BSP_FP8_E4M3, WS, ldws, 1, 7};
 }
-// Few tokens and a large weight: the CTAs of 16 outputs would each bring all tokens to 8 bits.  In one launch / quantised first (us): 8 tokens, 4096 x
-// 4096 6.4 / 6.2, 13 tokens 9.5 / 9.2, 32 tokens 16 / 8.2; smaller weights, 4096 x 1024 with 13 tokens 3.5 / 4.4, 32 tokens 5.9 / 5.8, 1024 x 1024 with 32
-// tokens 4.2 / 4.8.
-bool large_weight(int n_out, int k_in) { return static_cast<long long>(n_out) * k_in >= (8ll << 20); }
+// Whether the kernel for few tokens takes a product.  Its CTAs of 16 outputs each read all tokens, and bring them to 8 bits themselves if they are not
+// yet (ready).  Up to 8 tokens it is the fastest everywhere, up to 16 unless the weight is large, up to 32 only where it also saves the quantiser's
+// launch and the weight is small.  In one launch / quantised first, then on tensor cores (us): 16 tokens, 4096 x 1024 3.6 / 5.0, 2048 x 2048 4.3 / 4.9, 2048
+// x 4096 8.5 / 6.1, 4096 x 4096 9.8 / 7.8; 32 tokens, 768 x 768 4.2 / 4.6, 1024 x 1024 4.1 / 4.5, 512 x 2048 4.8 / 4.7, 4096 x 1024 5.8 / 5.0, 1024 x 4096 6.4 /
+// 5.9.  Ready, 24 tokens: 1024 x 1024 2.95 / 3.18, 512 x 2048 3.65 / 3.18, 4096 x 1024 3.96 / 3.76.
+bool few_is_faster(int tokens, int n_out, int k_in, bool ready) {
+  const long long weights = static_cast<long long>(n_out) * k_in;
+  return tokens <= 8 || (tokens <= 16 ? weights < (8ll << 20) : !ready && weights <= (1ll << 20));
+}
 int row_pitch(int k_in) { return (k_in - 1) / 16 * 16 + 16; }
 
 }  // namespace
@@ -106,7 +111,7 @@ extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* 
   const Product p{Operand{static_cast<const uint8_t*>(Xq), tokens, ldx, 0, fmt, XS, ldxs, 1, 0}, weight_operand(Wq, ldw, WS, ldws, n_out), k_in,
                   static_cast<uint16_t*>(Y), ldy, static_cast<const uint16_t*>(bias), act, nullptr, 1};
   if (n_out > kMostSize || k_in > kMostSize) return BSP_ERR_UNSUPPORTED;
-  if (few_tokens_ok(Wq, ldw, tokens) && aligned_to(Xq, 16) && ldx % 16 == 0 && (tokens <= 16 || !large_weight(n_out, k_in)))
+  if (few_tokens_ok(Wq, ldw, tokens) && aligned_to(Xq, 16) && ldx % 16 == 0 && few_is_faster(tokens, n_out, k_in, true))
     return launch_few_ready(p, static_cast<cudaStream_t>(stream));
   return run_product(p, static_cast<cudaStream_t>(stream));
 }
@@ -131,7 +136,7 @@ extern "C" int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ld
   BSP_TRY(bsp_linear_fp8_ws_bytes(tokens, k_in, &need));
   if (ws_bytes < need) return BSP_ERR_WORKSPACE;
   if (n_out > kMostSize) return BSP_ERR_UNSUPPORTED;
-  if (few_tokens_ok(Wq, ldw, tokens) && (tokens <= 8 || !large_weight(n_out, k_in)))
+  if (few_tokens_ok(Wq, ldw, tokens) && few_is_faster(tokens, n_out, k_in, false))
     return launch_few(Wq, ldw, WS, ldws, n_out, k_in, X, tokens, ldx, bias, act, Y, ldy, static_cast<cudaStream_t>(stream));
   uint8_t* Q = static_cast<uint8_t*>(ws);
   uint8_t* S = Q + static_cast<size_t>(tokens) * row_pitch(k_in);
