@@ -698,10 +698,15 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
   if (!(beta1 >= 0.0f && beta1 < 1.0f) || !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0.0f)) return BSP_ERR_ARG;
   if (step_dev == nullptr && step < 1) return BSP_ERR_ARG;
   if (!aligned_to(grad_scale, 4) || !aligned_to(step_dev, 4)) return BSP_ERR_ARG;
+  // one kernel for each kind of tensor, and launches of up to kAdamMaxJobs tensors of that kind
+  enum { kStream8, kAny8, kBits32, kKinds };
+  auto kind_of = [](const bsp_adam_job& a, const AdamJob& j) { return a.state_bits == 32 ? kBits32 : streams(a, j) ? kStream8 : kAny8; };
   AdamTable T;
+  int of_kind[kKinds] = {0, 0, 0};
   for (int i = 0; i < n_jobs; ++i) {                  // all jobs are checked before the first launch
     long long ctas;
     BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &T.job[0], &ctas));
+    ++of_kind[kind_of(jobs[i], T.job[0])];
   }
   TcDevice* dev = tc_device();
   if (dev == nullptr) return BSP_ERR_CUDA;
@@ -716,11 +721,9 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
   T.log_beta2 = static_cast<float>(log(static_cast<double>(beta2)));
   T.seed = seed; T.step = step; T.step_dev = step_dev; T.grad_scale = grad_scale;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // one kernel for each kind of tensor, and launches of up to kAdamMaxJobs tensors of that kind
-  enum { kStream8, kAny8, kBits32 };
   for (const int kind : {kStream8, kAny8, kBits32}) {
     if (kind != kBits32 && T.eps > 0.0f && T.eps < FLT_MIN) T.eps = FLT_MIN;     // (a denormal one has no reciprocal there)
-    for (int i = 0; i < n_jobs;) {
+    for (int i = 0; of_kind[kind] > 0 && i < n_jobs;) {
       long long total = 0;
       T.n_jobs = 0;
       T.g_size = 2;
@@ -728,13 +731,13 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
         AdamJob& j = T.job[T.n_jobs];
         long long ctas;
         BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &j, &ctas));
-        if (kind != (jobs[i].state_bits == 32 ? kBits32 : streams(jobs[i], j) ? kStream8 : kAny8)) continue;
+        if (kind != kind_of(jobs[i], j)) continue;
         if (T.n_jobs > 0 && total + ctas > 0x3fffffffLL) break;
         if (!j.grad16) T.g_size = 4;
         T.first[T.n_jobs++] = static_cast<int>(total);
         total += ctas;
       }
-      if (T.n_jobs == 0) break;
+      of_kind[kind] -= T.n_jobs;
       T.first[T.n_jobs] = static_cast<int>(total);
       if (kind == kStream8) {
         static OncePerDevice once;
