@@ -521,7 +521,8 @@ int bsp_linear_tune(const bsp_linear_call* call, int reps, int* best_route, floa
  * Outputs may have any alignment; they are stored fastest where they are 16-byte aligned with rows and leading dimensions of a
  * multiple of 8.  Bounded waits as bsp_linear_planned: check bsp_linear_status.
  * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE (leading dimension too small, block does not divide n_out), BSP_ERR_WORKSPACE,
- * BSP_ERR_UNSUPPORTED (a size beyond 2^31 - 512; bsp_fp8_quantize*: more than 65535 * 128 rows).
+ * BSP_ERR_UNSUPPORTED (a size beyond 2^31 - 512; bsp_fp8_quantize* and bsp_linear_fp8: more than 65535 * 128
+ * rows).
  * The kernel is chosen by size, so a row's last bits may differ between numbers of tokens; the same call gives the same bits.  Calls that
  * may run at the same time need a ws each. */
 typedef enum { BSP_FP8_E4M3 = 0, BSP_FP8_E5M2 = 1 } bsp_fp8_format;

@@ -475,6 +475,8 @@ def make_adam_job_array(jobs):
         for t in (j.m_scale, j.v_scale):
             if t is not None and (tuple(t.shape) != scales or not t.is_contiguous() or t.element_size() != 1):
                 raise ValueError(f"scales are contiguous bytes of shape {scales}")
+        if j.keep is not None and (j.keep.numel() * j.block != shape[0] * shape[1] or not j.keep.is_contiguous() or j.keep.element_size() != 1):
+            raise ValueError(f"keep is a contiguous byte for each group of {j.block} of {shape[0]} x {shape[1]} weights")
         a.W, a.rows, a.cols, a.ldw = _ptr(j.W), shape[0], shape[1], _ld(j.W)
         a.grad, a.ldg, a.grad_type = _ptr(j.grad), _ld(j.grad), GRAD_BF16 if j.grad.element_size() == 2 else GRAD_F32
         a.m, a.v, a.ldm, a.state_bits = _ptr(j.m), _ptr(j.v), _ld(j.m), 8 * j.m.element_size()

@@ -170,3 +170,11 @@ def test_adam_refuses_a_call():
 def test_descriptors_of_another_kind_are_refused():
     with pytest.raises(ctypes.ArgumentError):
         bsp.bsp_masked_adam_step_batched((binding._LayerJob * 1)(), 0.9, 0.999, 1e-8, 1, stream=0)
+
+
+@pytest.mark.parametrize("keep", [torch.ones(2, 16, dtype=torch.uint8), torch.ones(4, 15, dtype=torch.uint8), torch.ones(4, 32, dtype=torch.uint8)[:, ::2],
+                                  torch.ones(4, 16, dtype=torch.int16)])
+def test_flags_of_another_size_are_refused(keep):
+    w = torch.zeros(8, 16)
+    with pytest.raises(ValueError, match="keep is"):
+        bsp.make_adam_job_array([bsp.AdamJob(W=w, grad=w, m=w, v=w, lr=1.0, keep=keep, block=2)])
