@@ -252,6 +252,31 @@ def test_few_and_many_tiles(t, n, k, block, fmt):
     layer.backward_weight(True)
 
 
+@pytest.mark.parametrize("t,n,k", [(3, 256, 512), (40, 256, 512), (128, 512, 2304), (700, 1100, 700)])
+def test_weight_written_just_before(t, n, k):
+    """The weight is quantised anew ahead of every call, with nothing between them; so are X and the workspace used again."""
+    rng = np.random.default_rng(9)
+    weights = [to_dev(bf16_bits(rng.normal(size=(n, k)) * 2.0 ** i)) for i in range(4)]
+    X, bias = to_dev(random_matrix(rng, t, k, 1.0)), to_dev(bf16_bits(rng.normal(size=n)))
+    ws = torch.empty(bsp.bsp_linear_fp8_ws_bytes(t, k), dtype=torch.uint8, device=DEV)
+    Wq, WS = torch.empty((n, up(k, 16)), dtype=torch.uint8, device=DEV)[:, :k], torch.empty((up(n, 128) // 128, up(k, 128) // 128), dtype=torch.uint8, device=DEV)
+    out = [torch.zeros((t, n), dtype=torch.int16, device=DEV) for _ in range(64)]
+    ref = []
+    for W in weights:
+        bsp.bsp_fp8_quantize_weight(W, Wq, WS)
+        torch.cuda.synchronize()
+        bsp.bsp_linear_fp8(Wq, WS, X, bias, bsp.ACT_NONE, out[0], ws)
+        torch.cuda.synchronize()
+        ref.append(out[0].clone())
+    torch.cuda.synchronize()
+    for i, Y in enumerate(out):
+        bsp.bsp_fp8_quantize_weight(weights[i % 4], Wq, WS)
+        bsp.bsp_linear_fp8(Wq, WS, X, bias, bsp.ACT_NONE, Y, ws)
+    bsp.bsp_linear_status()
+    for i, Y in enumerate(out):
+        assert torch.equal(Y, ref[i % 4]), i
+
+
 def test_the_same_bits_every_time():
     """Split contractions are added in a fixed order, whichever CTA is ready first."""
     layer = Layer(130, 512, 4096, 3)
