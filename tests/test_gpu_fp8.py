@@ -277,6 +277,44 @@ def test_weight_written_just_before(t, n, k):
         assert torch.equal(Y, ref[i % 4]), i
 
 
+def test_weight_written_just_before_in_a_graph():
+    """The same in a captured graph, two layers of different routes one after the other, replayed with other weights in the same place."""
+    rng = np.random.default_rng(10)
+    shapes = [(40, 256, 512), (128, 512, 2304)]
+    layers = []
+    for t, n, k in shapes:
+        layers.append(dict(
+            W=to_dev(bf16_bits(rng.normal(size=(n, k)))), X=to_dev(random_matrix(rng, t, k, 1.0)),
+            ws=torch.empty(bsp.bsp_linear_fp8_ws_bytes(t, k), dtype=torch.uint8, device=DEV), Wq=torch.empty((n, k), dtype=torch.uint8, device=DEV),
+            WS=torch.empty((up(n, 128) // 128, up(k, 128) // 128), dtype=torch.uint8, device=DEV),
+            Y=[torch.zeros((t, n), dtype=torch.int16, device=DEV) for _ in range(4)]))
+
+    def step():
+        for i in range(4):
+            for L in layers:
+                bsp.bsp_fp8_quantize_weight(L["W"], L["Wq"], L["WS"])
+                bsp.bsp_linear_fp8(L["Wq"], L["WS"], L["X"], None, bsp.ACT_NONE, L["Y"][i], L["ws"])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(5):
+        new = [to_dev(bf16_bits(np.random.default_rng(seed).normal(size=L["W"].shape) * 2.0 ** seed)) for L in layers]
+        for L, w in zip(layers, new):
+            L["W"].copy_(w)
+        graph.replay()
+        bsp.bsp_linear_status()
+        got = [[y.clone() for y in L["Y"]] for L in layers]
+        for L, ys in zip(layers, got):
+            bsp.bsp_fp8_quantize_weight(L["W"], L["Wq"], L["WS"])
+            torch.cuda.synchronize()
+            bsp.bsp_linear_fp8(L["Wq"], L["WS"], L["X"], None, bsp.ACT_NONE, L["Y"][0], L["ws"])
+            torch.cuda.synchronize()
+            assert all(torch.equal(y, L["Y"][0]) for y in ys)
+
+
 def test_the_same_bits_every_time():
     """Split contractions are added in a fixed order, whichever CTA is ready first."""
     layer = Layer(130, 512, 4096, 3)
