@@ -732,15 +732,26 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
   if (!(beta1 >= 0.0f && beta1 < 1.0f) || !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0.0f)) return BSP_ERR_ARG;
   if (step_dev == nullptr && step < 1) return BSP_ERR_ARG;
   if (!aligned_to(grad_scale, 4) || !aligned_to(step_dev, 4)) return BSP_ERR_ARG;
-  // one kernel for each kind of tensor, and launches of up to kAdamMaxJobs tensors of that kind
+  // One kernel for each kind of tensor, and launches of up to kAdamMaxJobs tensors of that kind.  All jobs are checked before the first
+  // launch, and the first kAdamMaxJobs of them looked over only then.
   enum { kStream8, kAny8, kBits32, kKinds };
-  auto kind_of = [](const bsp_adam_job& a, const AdamJob& j) { return a.state_bits == 32 ? kBits32 : streams(a, j) ? kStream8 : kAny8; };
-  AdamTable T;
-  int of_kind[kKinds] = {0, 0, 0};
-  for (int i = 0; i < n_jobs; ++i) {                  // all jobs are checked before the first launch
+  struct Made {
+    AdamJob job;
+    int kind;
     long long ctas;
-    BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &T.job[0], &ctas));
-    ++of_kind[kind_of(jobs[i], T.job[0])];
+  };
+  auto make = [&](int i, Made* made) {
+    BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &made->job, &made->ctas));
+    made->kind = jobs[i].state_bits == 32 ? kBits32 : streams(jobs[i], made->job) ? kStream8 : kAny8;
+    return static_cast<int>(BSP_OK);
+  };
+  AdamTable T;
+  Made known[kAdamMaxJobs], other;
+  int of_kind[kKinds] = {0, 0, 0};
+  for (int i = 0; i < n_jobs; ++i) {
+    Made* made = i < kAdamMaxJobs ? &known[i] : &other;
+    BSP_TRY(make(i, made));
+    ++of_kind[made->kind];
   }
   TcDevice* dev = tc_device();
   if (dev == nullptr) return BSP_ERR_CUDA;
@@ -762,26 +773,39 @@ extern "C" int bsp_masked_adam_step_batched(const bsp_adam_job* jobs, int n_jobs
       T.n_jobs = 0;
       T.g_size = 2;
       for (; i < n_jobs && T.n_jobs < kAdamMaxJobs; ++i) {
-        AdamJob& j = T.job[T.n_jobs];
-        long long ctas;
-        BSP_TRY(make_job(jobs[i], static_cast<uint32_t>(i), &j, &ctas));
-        if (kind != kind_of(jobs[i], j)) continue;
-        if (T.n_jobs > 0 && total + ctas > 0x3fffffffLL) break;
-        if (!j.grad16) T.g_size = 4;
+        if (i >= kAdamMaxJobs) BSP_TRY(make(i, &other));
+        const Made& made = i < kAdamMaxJobs ? known[i] : other;
+        if (made.kind != kind) continue;
+        if (T.n_jobs > 0 && total + made.ctas > 0x3fffffffLL) break;
+        if (!made.job.grad16) T.g_size = 4;
+        T.job[T.n_jobs] = made.job;
         T.first[T.n_jobs++] = static_cast<int>(total);
-        total += ctas;
+        total += made.ctas;
       }
       of_kind[kind] -= T.n_jobs;
       T.first[T.n_jobs] = static_cast<int>(total);
+      // (the table by its address: 11 KB)
+      void* args[1] = {&T};
+      cudaLaunchConfig_t cfg = {};
+      cfg.blockDim = dim3(kAdamThreads);
+      cfg.stream = s;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      attr[0].val.programmaticStreamSerializationAllowed = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      const void* kernel = reinterpret_cast<const void*>(kind == kAny8 ? adam_batched8_kernel : adam_batched_kernel);
+      long long grid = total;
       if (kind == kStream8) {
         static OncePerDevice once;
-        const int smem = kStreamHead + kStreamStages * stream_stage(T.g_size);
         BSP_TRY(allow_dynamic_smem(once, adam_stream8_kernel, kStreamHead + kStreamStages * stream_stage(4)));
-        const long long grid = total < static_cast<long long>(kStreamCtas) * dev->sms ? total : static_cast<long long>(kStreamCtas) * dev->sms;
-        BSP_CUDA_TRY(launch_pdl(adam_stream8_kernel, dim3(static_cast<unsigned>(grid)), dim3(kAdamThreads), smem, s, T));
-      } else {
-        BSP_CUDA_TRY(launch_pdl(kind == kAny8 ? adam_batched8_kernel : adam_batched_kernel, dim3(static_cast<unsigned>(total)), dim3(kAdamThreads), 0, s, T));
+        cfg.dynamicSmemBytes = kStreamHead + kStreamStages * stream_stage(T.g_size);
+        kernel = reinterpret_cast<const void*>(adam_stream8_kernel);
+        const long long seats = static_cast<long long>(kStreamCtas) * dev->sms;
+        if (seats < grid) grid = seats;
       }
+      cfg.gridDim = dim3(static_cast<unsigned>(grid));
+      BSP_CUDA_TRY(cudaLaunchKernelExC(&cfg, kernel, args));
     }
     T.eps = eps;
   }
