@@ -82,11 +82,11 @@ __device__ __noinline__ uint4 load_some(const uint16_t* src, int n) {
   return make_uint4(static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32));
 }
 // A thread's rows x 16 columns of the tile, as pairs.
-template <bool kWhole, int ROWS>
+template <bool kWhole, int STEP, int ROWS>
 __device__ __forceinline__ void load_tile(const QuantArgs& A, int r0, int c, int n, uint32_t (&x)[ROWS][8]) {
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {           // evenly spread from this thread's first one on
-    const int r = r0 + kBlock / ROWS * i;
+    const int r = r0 + STEP * i;
     const uint16_t* src = A.X + static_cast<size_t>(r) * A.ldx + c;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -112,18 +112,24 @@ __device__ __forceinline__ uint32_t row_max(const uint32_t (&x)[8]) {
   return abs_max_of(m);
 }
 
-// Along the rows, or (kTile) with one scale for the tile.
-template <int FMT, bool kTile>
-__global__ void __launch_bounds__(kQuantThreads)
+// Along the rows, or (kTile) with one scale for the tile of 128 x 128.  Along the rows a CTA is 128 threads with 64 rows: 8192 registers, which
+// an SM has left beside a CTA of the products (bsp_gemm_fp8.cu).  With 256 threads neither could take its seat while the other ran: 1003 tokens, 4096 x 1024
+// 12.4 us for the whole layer, this way 11.4.  Up to 64 rows 256 threads share what there is (64 tokens, 1024 x 4096 6.3 and 6.8 us).
+constexpr int kSmallThreads = 128;
+template <int FMT, bool kTile, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 quantize_kernel(QuantArgs A) {
+  constexpr int kRows = THREADS / 2, kStep = kRows / 4;
+  static_assert(!kTile || kRows == kBlock, "a tile to a CTA");
   __shared__ uint32_t s_max[8];
   const int warp = threadIdx.x >> 5, l = threadIdx.x & 7, slot = threadIdx.x >> 3;   // eight threads to a row
-  const int r0 = blockIdx.y * kBlock + slot, c = blockIdx.x * kBlock + 16 * l;
+  const int col_blocks = blocks_of(A.cols), tile_r = static_cast<int>(blockIdx.x) / col_blocks, tile_c = static_cast<int>(blockIdx.x) - tile_r * col_blocks;
+  const int r0 = tile_r * kRows + slot, c = tile_c * kBlock + 16 * l;
   const int n = max(0, min(16, A.cols - c));   // of this thread's columns, those that exist
   pdl_wait();
   pdl_launch_dependents();
   uint32_t x[4][8];
-  load_tile<false>(A, r0, c, n, x);
+  load_tile<false, kStep>(A, r0, c, n, x);
   uint32_t tile = 0u;
   if (kTile) {
 #pragma unroll
@@ -138,12 +144,12 @@ quantize_kernel(QuantArgs A) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int r = r0 + 32 * i;
+    const int r = r0 + kStep * i;
     float inv;
     const uint32_t byte = block_scale<FMT>(kTile ? tile : row_max(x[i]), inv);
     if (r >= A.rows) continue;
     if (kTile ? threadIdx.x == 0 && i == 0 : l == 0)
-      A.s_row[static_cast<size_t>(kTile ? blockIdx.y : r) * A.lds_row + blockIdx.x] = static_cast<uint8_t>(byte);
+      A.s_row[static_cast<size_t>(kTile ? tile_r : r) * A.lds_row + tile_c] = static_cast<uint8_t>(byte);
     uint32_t q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) q[j] = four_to_fp8<FMT>(x[i][2 * j], x[i][2 * j + 1], inv, inv, inv, inv);
@@ -169,7 +175,7 @@ __device__ __forceinline__ void quantize_both(const QuantArgs& A, BothShared& s)
   const int r0 = blockIdx.y * kBlock + slot, c0 = blockIdx.x * kBlock, c = c0 + 16 * l;
   const int n = max(0, min(16, A.cols - c));
   uint32_t x[kRows][8];
-  load_tile<kWhole>(A, r0, c, n, x);
+  load_tile<kWhole, kStep>(A, r0, c, n, x);
   if (A.q_col != nullptr) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -327,8 +333,17 @@ extern "C" int bsp_fp8_quantize(const void* X, int rows, int cols, int ldx, int 
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const dim3 grid(blocks_of(cols), blocks_of(rows));
   const bool rows_only = Qc == nullptr && col_sums == nullptr;
-  auto kernel = fmt == BSP_FP8_E4M3 ? (rows_only ? quantize_kernel<BSP_FP8_E4M3, false> : quantize_both_kernel<BSP_FP8_E4M3>)
-                                    : (rows_only ? quantize_kernel<BSP_FP8_E5M2, false> : quantize_both_kernel<BSP_FP8_E5M2>);
+  if (rows_only) {
+    const int threads = rows <= kSmallThreads / 2 ? kQuantThreads : kSmallThreads;
+    const long long tiles = ((rows - 1ll) / (threads / 2) + 1) * grid.x;
+    if (tiles > 0x7fffffffll) return BSP_ERR_UNSUPPORTED;
+    auto rows_kernel = fmt == BSP_FP8_E4M3
+                           ? (threads == kSmallThreads ? quantize_kernel<BSP_FP8_E4M3, false, kSmallThreads> : quantize_kernel<BSP_FP8_E4M3, false, kQuantThreads>)
+                           : (threads == kSmallThreads ? quantize_kernel<BSP_FP8_E5M2, false, kSmallThreads> : quantize_kernel<BSP_FP8_E5M2, false, kQuantThreads>);
+    BSP_CUDA_TRY(launch_pdl(rows_kernel, dim3(static_cast<unsigned>(tiles)), dim3(threads), 0, s, A));
+    return BSP_OK;
+  }
+  auto kernel = fmt == BSP_FP8_E4M3 ? quantize_both_kernel<BSP_FP8_E4M3> : quantize_both_kernel<BSP_FP8_E5M2>;
   if (in_cluster) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -363,7 +378,9 @@ extern "C" int bsp_fp8_quantize_weight(const void* W, int n_out, int k_in, int l
   A.q_row = static_cast<uint8_t*>(Q); A.ld_row = ldq; A.s_row = S; A.lds_row = lds;
   A.wide_in = aligned_to(W, 16) && ldw % 8 == 0;
   A.wide_out = wide_stores(Q, ldq);
-  BSP_CUDA_TRY(launch_pdl(quantize_kernel<BSP_FP8_E4M3, true>, dim3(blocks_of(k_in), blocks_of(n_out)), dim3(kQuantThreads), 0,
+  const long long tiles = static_cast<long long>(blocks_of(k_in)) * blocks_of(n_out);
+  if (tiles > 0x7fffffffll) return BSP_ERR_UNSUPPORTED;
+  BSP_CUDA_TRY(launch_pdl(quantize_kernel<BSP_FP8_E4M3, true, kQuantThreads>, dim3(static_cast<unsigned>(tiles)), dim3(kQuantThreads), 0,
                           static_cast<cudaStream_t>(stream), A));
   return BSP_OK;
 }

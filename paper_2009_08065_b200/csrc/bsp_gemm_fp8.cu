@@ -92,11 +92,12 @@ __device__ __forceinline__ void finish_piece(const Fp8Params& P, uint32_t (&v)[3
 // The width is the launch's (choose_width): up to 240 two accumulators fit tensor memory beside the scales; a wider tile has one.
 // Every CTA holds the scales of its own rows of A and of all rows of B of the tile.
 // Roles per CTA: warps 0 and 11 TMA producers of A and B (completion is counted on the leader's mbarrier), warp 10 the scales, warp 1 of
-// the LEADER issues the MMAs and commits to both CTAs' barriers, warps 2 to 9 and 12 to 15 epilogue of the CTA's own 128 rows: three
-// groups of four.  (GELU is what they are for: 4096 x 4096 x 1024 takes 18.3 us without and 22.3 with it, which is then bound by the issue of its
-// arithmetic, not by the number of warps: 22.6 with two groups.)  No TMA multicast is used.  All mbarrier waits are bounded.
-constexpr int kFp8Threads = 512;
-constexpr int kEpiWarps = 12, kEpiGroups = kEpiWarps / 4;
+// the LEADER issues the MMAs and commits to both CTAs' barriers, warps 2 to 9 epilogue of the CTA's own 128 rows: two groups of four.  (With GELU
+// the issue of its arithmetic binds, 4096 x 4096 x 1024 18.3 us without and 22.3 with it, not the number of warps: with three groups the same.)
+// 384 threads of up to 140 registers leave room on the SM for a CTA of the quantiser (bsp_fp8_quantize.cu), which therefore starts
+// while these run, and these while it runs.  No TMA multicast is used.  All mbarrier waits are bounded.
+constexpr int kFp8Threads = 384;
+constexpr int kEpiWarps = 8, kEpiGroups = kEpiWarps / 4;
 constexpr int kPairStage = 2 * kBlockM * kBlock;           // 128 rows of A, up to 128 of B
 constexpr int kPairStages = 6;
 constexpr int kPairEpi = kEpiWarps * kWarpEpi;
@@ -377,7 +378,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     if (!ok && lane == 0) record_timeout(P.status, timed_out);
   } else if (warp >= 2) {
     // ---------------------------------------------------------------- epilogue of this CTA's 128 rows
-    const int number = warp < 10 ? warp - 2 : warp - 4;          // 0 to 11
+    const int number = warp - 2;                                 // 0 to 7
     const int group = number >> 2;
     const int quad = warp & 3;                                   // the quarter of tensor memory that the warp may read
     const int epi_tid = number * 32 + lane;
