@@ -606,7 +606,8 @@ adam_stream8_kernel(const __grid_constant__ AdamTable T) {
       rates(T, same, T.job[job], R);
     }
     const AdamJob& J = T.job[job];
-    if (!tc::mbar_wait(full + 8u * stage, phase, T.status)) { ok = false; break; }
+    // (one answer for the warp: its lanes meet again in what follows, so none may leave alone)
+    if (!tc::mbar_wait_warp(full + 8u * stage, phase, T.status)) { ok = false; break; }
     if (chunk + grid < chunks) look_up(chunk + grid);
     const uint32_t at_stage = base + stage * stage_bytes, number = static_cast<uint32_t>(chunk - T.first[job]);
     if (J.cols % kBlock != 0) chunk_step<true>(J, now, number, at_stage, R);

@@ -261,7 +261,7 @@ gemm_fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
   // ---------------------------------------------------------------- this CTA's columns
   if (epilogue) {
     epilogue_sync_all();                               // s_bias is complete
-    if (C > 1 && !mbar_wait(recv_bar, 0u, P.status)) {
+    if (C > 1 && !mbar_wait_warp(recv_bar, 0u, P.status)) {     // (one answer for the warp, which lane 0 records)
       if (lane == 0) record_timeout(P.status, timed_out);
       ok = false;
     }

@@ -235,7 +235,7 @@ gemm_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   // ---------------------------------------------------------------- this CTA's columns
   if (epilogue) {
     if constexpr (!kTmaStore) epilogue_sync_all();     // s_bias is complete (with TMA stores: the vote below)
-    if (!mbar_wait(recv_bar, 0u, P.status)) {
+    if (!mbar_wait_warp(recv_bar, 0u, P.status)) {     // (one answer for the warp, which lane 0 records)
       if (lane == 0) record_timeout(P.status, timed_out);
       ok = false;
     }

@@ -1,0 +1,43 @@
+"""Source rules of the kernels' waits and barriers: what no run can show, because it takes a wait that expires in one lane of a warp
+only, or a compiler that leaves a warp split."""
+import glob
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2009_08065_b200", "csrc")
+SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+
+
+def source(path):
+    src = open(os.path.join(CSRC, path)).read()
+    return re.sub(r"//[^\n]*", "", re.sub(r"/\*.*?\*/", "", src, flags=re.S))
+
+
+def closing(src, at, pair="()"):
+    depth = 0
+    for i in range(at, len(src)):
+        depth += (src[i] == pair[0]) - (src[i] == pair[1])
+        if depth == 0:
+            return i
+    raise AssertionError("unbalanced")
+
+
+# Waits whose answer may differ between the lanes of a warp: each is the argument of a vote, or one thread's alone.
+VOTES = r"(?:__all_sync|__syncthreads_and|\w*_all_ok|epilogue_agree)\([^;{}]*$"
+
+
+@pytest.mark.parametrize("path", [os.path.basename(p) for p in SOURCES])
+def test_a_warp_leaves_a_bounded_wait_as_a_whole(path):
+    """A lane that gave up alone would leave the others at the next __syncwarp or vote, which then never ends."""
+    src = source(path)
+    for m in re.finditer(r"\bmbar_wait(?:_suspended)?\(", src):
+        before = src[:m.start()]
+        line = before[before.rindex("\n") + 1:]
+        if re.search(VOTES, line):
+            continue
+        enclosing = before[max(0, m.start() - 700):]
+        one_thread = "lane == 0" in enclosing[enclosing.rfind("if (warp"):].split("{")[0]
+        answered = "auto read_ticket = " in enclosing and "epilogue_all_ok(tile != -2)" in src
+        assert one_thread or answered, f"{path}: {line.strip()}{src[m.start():m.end() + 40]}"
