@@ -83,6 +83,7 @@ __device__ __forceinline__ void finish_piece(const Fp8Params& P, uint32_t (&v)[3
         if (e < n) dst[static_cast<size_t>(8 * i) * P.ldy + e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
     }
   }
+  __syncwarp();                                    // (what follows reads tensor memory, which takes the whole warp at once)
 }
 
 // Two CTAs of a cluster share a tile of 256 x w outputs, as in bsp_linear_tc2.cu: each loads its own 128 rows of A and half of the
@@ -156,7 +157,10 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar_cluster) {
 }
 
 // Named barriers of the epilogue warps; the second with an AND reduction: whether all of their waits succeeded.
-__device__ __forceinline__ void epilogue_meet() { asm volatile("bar.sync 3, %0;" ::"n"(32 * kEpiWarps) : "memory"); }
+__device__ __forceinline__ void epilogue_meet() {
+  __syncwarp();
+  asm volatile("bar.sync 3, %0;" ::"n"(32 * kEpiWarps) : "memory");
+}
 __device__ __forceinline__ bool epilogue_agree(bool ok) {
   uint32_t r;
   asm volatile(

@@ -432,10 +432,10 @@ select_kernel(const __grid_constant__ SelectBatchT<N> B) {
   const uint32_t* keys = reinterpret_cast<const uint32_t*>(J.S);
   const long long n = J.n;
   if (threadIdx.x == 0) s_n = s_last_n = 0u;
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  tc::cluster_arrive_relaxed();
   pdl_wait();
   pdl_launch_dependents();
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");   // every CTA of the cluster has started
+  tc::cluster_wait();                                        // every CTA of the cluster has started
   if (J.r <= 0) {                                            // the same for the whole cluster
     if (rank == 0 && threadIdx.x == 0) *J.out = -1.0f;
     return;

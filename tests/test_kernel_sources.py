@@ -41,3 +41,20 @@ def test_a_warp_leaves_a_bounded_wait_as_a_whole(path):
         one_thread = "lane == 0" in enclosing[enclosing.rfind("if (warp"):].split("{")[0]
         answered = "auto read_ticket = " in enclosing and "epilogue_all_ok(tile != -2)" in src
         assert one_thread or answered, f"{path}: {line.strip()}{src[m.start():m.end() + 40]}"
+
+
+@pytest.mark.parametrize("path", [os.path.basename(p) for p in SOURCES + glob.glob(os.path.join(CSRC, "*.cuh"))])
+def test_cluster_barriers_take_the_whole_warp(path):
+    """The aligned forms are undefined for part of a warp: each stands right behind a __syncwarp()."""
+    src = source(path)
+    for m in re.finditer(r"asm volatile\(\s*\"barrier\.cluster\.", src):
+        assert src[:m.start()].rstrip().endswith("__syncwarp();"), f"{path}: {src[m.start():m.end() + 40]}"
+
+
+def test_tensor_memory_is_read_by_the_whole_warp():
+    """The pair kernel's stores go by lanes; what follows them in its loop reads tensor memory and meets at named barriers."""
+    src = source("bsp_gemm_fp8.cu")
+    at = src.index("{", src.index("void finish_piece("))
+    assert src[at:closing(src, at, "{}")].rstrip().endswith("__syncwarp();")
+    at = src.index("{", src.index("void epilogue_meet("))
+    assert src[at + 1:].lstrip().startswith("__syncwarp();")
