@@ -172,8 +172,7 @@ inline int sm_count(int* sms) {
 // started knows that everything BEFORE that predecessor is complete, though not the predecessor itself; and once
 // its own pdl_wait returns, that too.  Hence global memory is touched after pdl_wait, except for
 //   - data older than the direct predecessor, where the library itself launched that predecessor: W and the sums
-//     behind the percentile's clearing kernel (bsp_select.cu), W in the second packing stage (bsp_fused.cu), the weight
-//     of an 8-bit linear layer behind the quantiser of its activations (bsp_linear_fp8.cu);
+//     behind the percentile's clearing kernel (bsp_select.cu), W in the second packing stage (bsp_fused.cu);
 //   - the weights of a plan that the caller vouches for (BSP_LINEAR_PLAN_STABLE): the weight warp of
 //     linear_tc_kernel, gemm_pair_kernel and gemm_split_kernel, which does not wait and therefore does not signal either.
 // A kernel that allocates tensor memory signals behind its allocation: a dependent CTA that took the memory first would wait for

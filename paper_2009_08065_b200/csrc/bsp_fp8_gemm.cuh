@@ -15,7 +15,6 @@ struct Product {
   int act;
   const uint8_t* keep;       // flags [A.rows / block, B.rows], or null
   int block;
-  bool b_older = false;      // B and its scales are older than the launch before this one, which is the library's own (see launch_pdl)
 };
 
 // bsp_gemm_fp8.cu: operands whose rows begin at multiples of 16 bytes.

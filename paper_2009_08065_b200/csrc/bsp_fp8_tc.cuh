@@ -36,9 +36,7 @@ struct Scales {
     if (FORM == ScaleForm::kTiles) {
       // at most two different scales for a block: one byte per lane
       const int first = row0 >> O.s_shift, last = (O.rows - 1) >> O.s_shift;
-      // (from L2: a weight's scales may be read ahead of pdl_wait, see Product, and the launch before last may have written them)
-      const uint8_t* p = O.s + min(first + ((lane >> 3) & 1), last) * O.s_row + (block0 + min(lane & 7, n - 1)) * O.s_k;
-      asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(x[0]) : "l"(p) : "memory");
+      x[0] = ld_global(O.s + min(first + ((lane >> 3) & 1), last) * O.s_row + (block0 + min(lane & 7, n - 1)) * O.s_k);
     } else if (FORM == ScaleForm::kRows) {               // lane l: rows l, l + 32, l + 64, l + 96
       const bool wide = ((reinterpret_cast<uintptr_t>(O.s) | static_cast<uintptr_t>(O.s_row) | static_cast<uintptr_t>(block0)) & 7u) == 0;
 #pragma unroll

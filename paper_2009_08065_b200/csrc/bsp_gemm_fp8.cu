@@ -34,7 +34,6 @@ struct Fp8Params {
   int block, keep_wide;      // eight flags at a time
   uint16_t* Y;
   int ldy, y_wide;           // 16-byte stores
-  int b_older;               // see Product
   int* status;
 };
 
@@ -228,14 +227,11 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const int k_blocks = blocks_of(P.contraction);
   const int accs = pair_accumulators(w);
   const int tiles_b = (w + 127) >> 7;                  // sets of 128 rows of B with scales
-  // Before this returns nothing of global memory is touched (but B where it is older), and nothing signalled across the pair.  Each role calls it
-  // where it has computed all it can: the kernel before is mostly still running, and what comes behind it costs up to 0.5 us in instructions that are
-  // not cached yet.
-  auto begin_work = [&](bool older = false) {
-    if (!older) {
-      pdl_wait();
-      pdl_launch_dependents();
-    }
+  // Before this returns nothing of global memory is touched, and nothing signalled across the pair.  Each role calls it where it has computed
+  // all it can: the kernel before is mostly still running, and what comes behind it costs up to 0.5 us in instructions that are not cached yet.
+  auto begin_work = [&] {
+    pdl_wait();
+    pdl_launch_dependents();
     cluster_wait();              // the other CTA's barriers exist, and its tensor memory is allocated
   };
 
@@ -255,7 +251,7 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     };
     int row0 = first_row(pair);
     keep_here(row0);
-    begin_work(!for_a && P.b_older != 0);
+    begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
       if (tile != pair) row0 = first_row(tile);
       for (int kb = 0; kb < k_blocks; ++kb) {
@@ -281,12 +277,6 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     int m0 = (pair / n_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0 = (pair % n_tiles) * w;
     keep_here(m0);
     keep_here(n0);
-    ScalesB<kAMn> y, z;
-    const bool early = P.b_older != 0;
-    if (early) {
-      y.load(P.B, n0, 0, min(4, k_blocks), lane);
-      if (tiles_b > 1) z.load(P.B, n0 + 128, 0, min(4, k_blocks), lane);
-    }
     begin_work();
     for (int tile = pair; tile < total_tiles && ok; tile += n_pairs) {
       if (tile != pair) {
@@ -297,11 +287,10 @@ gemm_fp8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         const bool begin = tile == pair && kb == 0;
         const int n = min(begin ? 4 : 4 * kSlotGroups, k_blocks - kb);
         ScalesA<kAMn> x;
+        ScalesB<kAMn> y, z;
         x.load(P.A, m0, kb, n, lane);
-        if (!begin || !early) {
-          y.load(P.B, n0, kb, n, lane);
-          if (tiles_b > 1) z.load(P.B, n0 + 128, kb, n, lane);
-        }
+        y.load(P.B, n0, kb, n, lane);
+        if (tiles_b > 1) z.load(P.B, n0 + 128, kb, n, lane);
         ok = mbar_wait_warp(scale_empty_bar(slot), phase ^ 1u, P.status);
         if (!ok) break;
         uint32_t dst = smem_base + kScalesOff + slot * kSlotGroups * kPairScaleGroup;
@@ -462,7 +451,7 @@ int launch_pair(const Product& p, int w, TcDevice* dev, cudaStream_t s) {
       !(kBMn ? make_map8(&map_b, p.B.q, p.B.rows, p.contraction, p.B.ld, kBlock) : make_map8(&map_b, p.B.q, p.contraction, p.B.rows, p.B.ld, b_rows)))
     return BSP_ERR_CUDA;
   const Fp8Params P{p.A, p.B, p.contraction, a_rows * kBlock, b_rows * kBlock, w, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, 256, w), p.act, p.bias,
-                    p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, p.b_older, dev->status};
+                    p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, dev->status};
   const long long tiles = static_cast<long long>((p.A.rows - 1) / 256 + 1) * ((p.B.rows - 1) / w + 1);
   const int pairs = tiles < dev->sms / 2 ? static_cast<int>(tiles) : dev->sms / 2;
   cudaLaunchConfig_t cfg = {};

@@ -37,7 +37,6 @@ struct Split8Params {
   int block, keep_wide;
   uint16_t* Y;
   int ldy, y_wide;
-  int b_older;               // see Product
   int* status;
 };
 
@@ -134,13 +133,12 @@ gemm_fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     }
     __syncwarp();
     asm volatile("bar.sync 6, 64;" ::: "memory");
-    if (!P.b_older) pdl_wait();
+    pdl_wait();
     for (int i = 0; i < ahead; ++i) load_b(i, i);
   } else if (warp == 11) {
-    if (!P.b_older) pdl_wait();
-    scales_b.load(P.B, n0, kb0, min(kTurn, n_blocks), lane);
-    if (P.b_older) pdl_wait();
+    pdl_wait();
     scales_a.load(P.A, m0, kb0, min(kTurn, n_blocks), lane);
+    scales_b.load(P.B, n0, kb0, min(kTurn, n_blocks), lane);
   } else if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -347,7 +345,7 @@ int launch_split8(const Product& p, TcDevice* dev, cudaStream_t s) {
   int tail_off = recv_off + kReceive;
   if (tail_off < kSmemLimit / 2 + 1024) tail_off = kSmemLimit / 2 + 1024;                // one CTA per SM
   const Split8Params P{p.A, p.B, n_tiles, k_blocks, stages, a_rows * kBlock, b_rows * kBlock, recv_off, tail_off, idesc_scaled(p.A.fmt, p.B.fmt, kAMn, kBMn, kBlockM, kTileN), p.act, p.bias,
-                       p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, p.b_older, dev->status};
+                       p.keep, p.block, aligned_to(p.keep, 8) && p.B.rows % 8 == 0, p.Y, p.ldy, aligned_to(p.Y, 16) && p.ldy % 8 == 0, dev->status};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(((p.A.rows - 1) / kBlockM + 1) * n_tiles * C);
   cfg.blockDim = dim3(kSplit8Threads);

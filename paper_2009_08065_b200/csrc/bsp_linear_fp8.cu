@@ -101,29 +101,19 @@ int row_pitch(int k_in) { return (k_in - 1) / 16 * 16 + 16; }
 }  // namespace
 }  // namespace bsp
 
-namespace bsp {
-namespace {
-
-int linear_quantized(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* Xq, int ldx, const uint8_t* XS, int ldxs, int fmt,
-                     int tokens, const void* bias, int act, void* Y, int ldy, bool weight_older, void* stream) {
+extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* Xq, int ldx,
+                                        const uint8_t* XS, int ldxs, int fmt, int tokens, const void* bias, int act, void* Y, int ldy, void* stream) {
+  using namespace bsp;
   BSP_TRY(check_weight(Wq, ldw, WS, ldws, n_out, k_in));
   if (Xq == nullptr || XS == nullptr || Y == nullptr || tokens <= 0 || !known_format(fmt)) return BSP_ERR_ARG;
   if ((act != BSP_ACT_NONE && act != BSP_ACT_GELU) || !aligned_to(Y, 2) || !aligned_to(bias, 2)) return BSP_ERR_ARG;
   if (ldx < k_in || ldxs < blocks_of(k_in) || ldy < n_out) return BSP_ERR_SHAPE;
   const Product p{Operand{static_cast<const uint8_t*>(Xq), tokens, ldx, 0, fmt, XS, ldxs, 1, 0}, weight_operand(Wq, ldw, WS, ldws, n_out), k_in,
-                  static_cast<uint16_t*>(Y), ldy, static_cast<const uint16_t*>(bias), act, nullptr, 1, weight_older};
+                  static_cast<uint16_t*>(Y), ldy, static_cast<const uint16_t*>(bias), act, nullptr, 1};
   if (n_out > kMostSize || k_in > kMostSize) return BSP_ERR_UNSUPPORTED;
   if (few_tokens_ok(Wq, ldw, tokens) && aligned_to(Xq, 16) && ldx % 16 == 0 && few_is_faster(tokens, n_out, k_in, true))
     return launch_few_ready(p, static_cast<cudaStream_t>(stream));
   return run_product(p, static_cast<cudaStream_t>(stream));
-}
-
-}  // namespace
-}  // namespace bsp
-
-extern "C" int bsp_linear_fp8_quantized(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* Xq, int ldx,
-                                        const uint8_t* XS, int ldxs, int fmt, int tokens, const void* bias, int act, void* Y, int ldy, void* stream) {
-  return bsp::linear_quantized(Wq, ldw, WS, ldws, n_out, k_in, Xq, ldx, XS, ldxs, fmt, tokens, bias, act, Y, ldy, false, stream);
 }
 
 extern "C" int bsp_linear_fp8_ws_bytes(int tokens, int k_in, size_t* bytes) {
@@ -152,8 +142,8 @@ extern "C" int bsp_linear_fp8(const void* Wq, int ldw, const uint8_t* WS, int ld
   uint8_t* S = Q + static_cast<size_t>(tokens) * row_pitch(k_in);
   BSP_TRY(bsp_fp8_quantize(X, tokens, k_in, ldx, BSP_FP8_E4M3, Q, row_pitch(k_in), S, blocks_of(k_in), nullptr, 0, nullptr, 0, nullptr, nullptr, 0,
                            stream));
-  // the launch before the product is the quantiser's, which does not write the weight
-  return linear_quantized(Wq, ldw, WS, ldws, n_out, k_in, Q, row_pitch(k_in), S, blocks_of(k_in), BSP_FP8_E4M3, tokens, bias, act, Y, ldy, true, stream);
+  return bsp_linear_fp8_quantized(Wq, ldw, WS, ldws, n_out, k_in, Q, row_pitch(k_in), S, blocks_of(k_in), BSP_FP8_E4M3, tokens, bias, act, Y, ldy,
+                                  stream);
 }
 
 extern "C" int bsp_linear_fp8_backward_input(const void* Wq, int ldw, const uint8_t* WS, int ldws, int n_out, int k_in, const void* dYq, int ldy,

@@ -58,3 +58,19 @@ def test_tensor_memory_is_read_by_the_whole_warp():
     assert src[at:closing(src, at, "{}")].rstrip().endswith("__syncwarp();")
     at = src.index("{", src.index("void epilogue_meet("))
     assert src[at + 1:].lstrip().startswith("__syncwarp();")
+
+
+@pytest.mark.parametrize("path", [os.path.basename(p) for p in SOURCES if "fp8" in p])
+def test_nothing_is_read_ahead_of_the_wait(path):
+    """The 8-bit kernels touch global memory only behind the wait for the launch before them, the operands too: which launch that is
+    is not theirs to know (another host thread may have put one that rewrites the weight between a quantiser and its product)."""
+    src = source(path)
+    for m in re.finditer(r"\bif\s*\(([^;{}]*)\)\s*\{?\s*pdl_wait\(\)", src):
+        assert re.fullmatch(r"warp [=<>]=? \d+(?: && warp < \d+)?", m.group(1)), f"{path}: a wait that not every call makes: {m.group(0)}"
+    assert not re.search(r"\b(?:pdl_wait|begin_work)\([^)]", src), f"{path}: a wait that not every call makes"
+    # the kernel that shares a contraction fills its first stages ahead of the CTA's meeting: in each such role the wait comes first
+    firsts = list(re.finditer(r"load_[ab]\(i, i\)|scales_[ab]\.load\(P\.[AB], [mn]0, kb0, min", src))
+    assert len(firsts) == (4 if "split" in path else 0)
+    for m in firsts:
+        role = src[:m.start()].rindex("if (warp ==")
+        assert "pdl_wait();" in src[role:m.start()], f"{path}: {m.group(0)}"
