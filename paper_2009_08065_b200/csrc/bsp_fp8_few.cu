@@ -121,13 +121,13 @@ linear_few_kernel(FewArgs A) {
     return q;
   };
   auto multiply = [&](const Block& q) {
-    const float scale_w = scale_value(q.scale);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
-      float c[4] = {0.0f, 0.0f, 0.0f, 0.0f}, scale_x;
+      float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      uint32_t scale_x;                      // as a byte
       uint4 v[2];                            // the token's values in 8 bits
       if constexpr (kReady) {
-        scale_x = scale_value(q.scale_x[j]);
+        scale_x = q.scale_x[j];
         v[0] = q.x[j][0][0];
         v[1] = q.x[j][1][0];
       } else {
@@ -140,7 +140,7 @@ linear_few_kernel(FewArgs A) {
         m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = abs_max2(m, __shfl_xor_sync(0xffffffffu, m, 2));
         float inv;
-        scale_x = scale_value(block_scale<FMT>(abs_max_of(m), inv));
+        scale_x = block_scale<FMT>(abs_max_of(m), inv);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           v[h] = make_uint4(four_to_fp8<FMT>(x[h][0].x, x[h][0].y, inv, inv, inv, inv), four_to_fp8<FMT>(x[h][0].z, x[h][0].w, inv, inv, inv, inv),
@@ -152,11 +152,15 @@ linear_few_kernel(FewArgs A) {
         mma_fp8<FMT>(c, q.w[h][0].z, q.w[h][1].z, q.w[h][0].w, q.w[h][1].w, v[h].z, v[h].w);
       }
       // this lane's outputs are of tokens 2 t and 2 t + 1 of the group
-      const float s0 = scale_w * __shfl_sync(0xffffffffu, scale_x, 8 * t), s1 = scale_w * __shfl_sync(0xffffffffu, scale_x, 8 * t + 4);
-      acc[j][0] = __fmaf_rn(c[0], s0, acc[j][0]);
-      acc[j][1] = __fmaf_rn(c[1], s1, acc[j][1]);
-      acc[j][2] = __fmaf_rn(c[2], s0, acc[j][2]);
-      acc[j][3] = __fmaf_rn(c[3], s1, acc[j][3]);
+      // (The product of two scales can lie outside float32's range where what it multiplies brings it back, or is zero: two factors of half
+      // its exponent each.)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t both = q.scale + __shfl_sync(0xffffffffu, scale_x, 8 * t + 4 * u), half = both >> 1;
+        const float s0 = scale_value(half), s1 = scale_value(both - half);
+        acc[j][u] = __fmaf_rn(c[u] * s0, s1, acc[j][u]);
+        acc[j][2 + u] = __fmaf_rn(c[2 + u] * s0, s1, acc[j][2 + u]);
+      }
     }
   };
   // the contraction's blocks are dealt to the warps of all CTAs of the cluster
