@@ -552,7 +552,8 @@ int bsp_linear_fp8_backward_weight(const void* dYq, int ldy, const uint8_t* dYS,
  *     128 neighbouring weights of a row, as in the form along rows above.  Zero bytes throughout are zero moments.  W is updated from the
  *     new moments in float32; these are then rounded to one of their two neighbours with the distance as probability,
  *     16 random bits each, a hash of (seed, step, number of the job in the array, position in the tensor): the same call
- *     gives the same bits.  A positive v is never rounded to zero.  A block whose new moments hold an infinity or a NaN becomes NaN.
+ *     gives the same bits.  A positive v is never rounded to zero.  A block whose new moments hold an infinity or a NaN at a kept
+ *     place becomes NaN; at a pruned place where either of the two is not finite, both begin again at zero.
  * grad_scale: device float that multiplies every gradient (clipping), or NULL.  step >= 1; if step_dev is not NULL the step is read from there
  * instead (it has to be at least 1 when the call runs), so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step.
  * Any shape and alignment; 16-byte accesses where pointers and leading dimensions allow them.  No two jobs may share memory that either writes.
