@@ -434,10 +434,17 @@ def bsp_linear_fp8_backward_weight(dYq: torch.Tensor, dYS: torch.Tensor, fmt_dy:
            "bsp_linear_fp8_backward_weight")
 
 
+# Element types that are taken: the one that is meant, or whole numbers of its size as its bits.
+_FLOAT32 = (torch.float32,)
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+_E4M3, _E5M2 = (torch.float8_e4m3fn, torch.uint8, torch.int8), (torch.float8_e5m2, torch.uint8, torch.int8)
+_SCALE, _FLAGS = (torch.uint8, torch.int8, torch.float8_e8m0fnu), (torch.uint8, torch.int8, torch.bool)
+
+
 @dataclass
 class AdamJob:
     """One tensor of a bsp_masked_adam_step_batched call: W float32 [rows, cols] (a bias: [1, cols]), grad float32 or bf16;
-    m, v float32, or 8-bit values (uint8 or torch's float8 types) with m_scale, v_scale uint8 [rows, ceil(cols / 128)]."""
+    m, v float32, or 8-bit values (m e4m3, v e5m2, or their bits as uint8) with m_scale, v_scale uint8 [rows, ceil(cols / 128)]."""
     W: torch.Tensor
     grad: torch.Tensor
     m: torch.Tensor
@@ -464,18 +471,18 @@ def make_adam_job_array(jobs):
         for t in (j.grad, j.m, j.v, j.W_bf16):
             if t is not None and tuple(t.shape) != shape:
                 raise ValueError(f"tensors of one job have shapes {shape} and {tuple(t.shape)}")
-        for t, size in ((j.W, 4), (j.m, j.v.element_size()), (j.W_bf16, 2)):
-            if t is not None and t.element_size() != size:
-                raise ValueError(f"unexpected element type {t.dtype}")
-        if j.m.element_size() not in (1, 4) or j.grad.element_size() not in (2, 4):
-            raise ValueError(f"unexpected element types {j.m.dtype}, {j.grad.dtype}")
+        moments = (_FLOAT32, _FLOAT32) if j.m.dtype in _FLOAT32 else (_E4M3, _E5M2)
+        for name, t, types in (("W", j.W, _FLOAT32), ("grad", j.grad, _FLOAT32 + _BF16), ("m", j.m, moments[0]), ("v", j.v, moments[1]),
+                               ("W_bf16", j.W_bf16, _BF16), ("m_scale", j.m_scale, _SCALE), ("v_scale", j.v_scale, _SCALE)):
+            if t is not None and t.dtype not in types:
+                raise ValueError(f"unexpected element type of {name}: {t.dtype}")
         if _ld(j.m) != _ld(j.v):
             raise ValueError("m and v have different leading dimensions")
         scales = (shape[0], (shape[1] + 127) // 128)
         for t in (j.m_scale, j.v_scale):
-            if t is not None and (tuple(t.shape) != scales or not t.is_contiguous() or t.element_size() != 1):
+            if t is not None and (tuple(t.shape) != scales or not t.is_contiguous()):
                 raise ValueError(f"scales are contiguous bytes of shape {scales}")
-        if j.keep is not None and (j.keep.numel() * j.block != shape[0] * shape[1] or not j.keep.is_contiguous() or j.keep.element_size() != 1):
+        if j.keep is not None and (j.keep.numel() * j.block != shape[0] * shape[1] or not j.keep.is_contiguous() or j.keep.dtype not in _FLAGS):
             raise ValueError(f"keep is a contiguous byte for each group of {j.block} of {shape[0]} x {shape[1]} weights")
         a.W, a.rows, a.cols, a.ldw = _ptr(j.W), shape[0], shape[1], _ld(j.W)
         a.grad, a.ldg, a.grad_type = _ptr(j.grad), _ld(j.grad), GRAD_BF16 if j.grad.element_size() == 2 else GRAD_F32

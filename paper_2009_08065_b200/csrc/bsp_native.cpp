@@ -15,6 +15,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "bsp.h"
 
@@ -60,21 +61,35 @@ class Args {
   static void want_shape(const Matrix& m, int rows, int cols) {
     TORCH_CHECK_VALUE(m.rows == rows && m.cols == cols, "expected a tensor of shape [", rows, ", ", cols, "], got [", m.rows, ", ", m.cols, "]");
   }
-  void want_bytes(int i, size_t size) const {
-    TORCH_CHECK_VALUE(tensor(i).element_size() == static_cast<int64_t>(size), "expected elements of ", size, " bytes, got ", tensor(i).scalar_type());
+  // Element types: the one that is meant, or whole numbers of its size as its bits.  (Another floating-point type of the same size would be
+  // read as values that it does not hold.)
+  using Type = at::ScalarType;
+  void want_type(int i, std::initializer_list<Type> types) const {
+    const Type type = tensor(i).scalar_type();
+    TORCH_CHECK_VALUE(std::find(types.begin(), types.end(), type) != types.end(), "expected elements of type ", *types.begin(), ", got ", type);
   }
+  void want_bf16(int i) const { want_type(i, {Type::BFloat16, Type::Short, Type::UInt16}); }
+  void want_fp8(int i, int fmt) const {
+    want_type(i, {fmt == BSP_FP8_E5M2 ? Type::Float8_e5m2 : Type::Float8_e4m3fn, Type::Byte, Type::Char});
+  }
+  void want_flags(int i) const { want_type(i, {Type::Byte, Type::Char, Type::Bool}); }
   // A contiguous tensor of `n` values.
-  void want_values(int i, long long n, size_t size) const {
+  void want_values(int i, long long n) const {
     TORCH_CHECK_VALUE(tensor(i).numel() == n && tensor(i).is_contiguous(), "expected a contiguous tensor of ", n, " values");
-    want_bytes(i, size);
   }
-  // 8-bit values of a matrix of X's shape, and scale bytes of a given one; nothing for None.
-  Matrix matrix_like(int i, const Matrix& X) const { return scales(i, X.rows, X.cols); }
+  // 8-bit values, and scale bytes, of a matrix of a given shape; nothing for None.
+  Matrix values8(int i, int rows, int cols, int fmt) const {
+    if (a_[i] == Py_None) return Matrix{nullptr, 0, 0, 0};
+    const Matrix m = matrix(i);
+    want_shape(m, rows, cols);
+    want_fp8(i, fmt);
+    return m;
+  }
   Matrix scales(int i, int rows, int cols) const {
     if (a_[i] == Py_None) return Matrix{nullptr, 0, 0, 0};
     const Matrix m = matrix(i);
     want_shape(m, rows, cols);
-    want_bytes(i, 1);
+    want_type(i, {Type::Byte, Type::Char, Type::Float8_e8m0fnu});
     return m;
   }
   long long integer(int i) const {
@@ -350,12 +365,15 @@ NATIVE(linear_run) {
 NATIVE(fp8_quantize) {
   NATIVE_ARGS(fp8_quantize, 9);
   A.one_device();
-  const Matrix X = A.matrix(0), Q = A.matrix_like(2, X), S = A.scales(3, X.rows, blocks(X.cols));
-  const Matrix Qc = A.matrix_like(4, X), Sc = A.scales(5, blocks(X.rows), X.cols);
-  A.want_bytes(0, 2);
   const int fmt = A.i32(1);
+  const Matrix X = A.matrix(0), Q = A.values8(2, X.rows, X.cols, fmt), S = A.scales(3, X.rows, blocks(X.cols));
+  const Matrix Qc = A.values8(4, X.rows, X.cols, fmt), Sc = A.scales(5, blocks(X.rows), X.cols);
+  A.want_bf16(0);
   float* sums = A.ptr<float>(6);
-  if (sums != nullptr) A.want_values(6, X.cols, 4);
+  if (sums != nullptr) {
+    A.want_values(6, X.cols);
+    A.want_type(6, {Args::Type::Float});
+  }
   void* ws = A.ptr(7);
   const size_t wsb = A.bytes(7);
   void* s = A.stream(8);
@@ -370,8 +388,8 @@ NATIVE(fp8_quantize) {
 NATIVE(fp8_quantize_weight) {
   NATIVE_ARGS(fp8_quantize_weight, 4);
   A.one_device();
-  const Matrix W = A.matrix(0), Q = A.matrix_like(1, W), S = A.scales(2, blocks(W.rows), blocks(W.cols));
-  A.want_bytes(0, 2);
+  const Matrix W = A.matrix(0), Q = A.values8(1, W.rows, W.cols, BSP_FP8_E4M3), S = A.scales(2, blocks(W.rows), blocks(W.cols));
+  A.want_bf16(0);
   void* s = A.stream(3);
   return status_of([&] { return bsp_fp8_quantize_weight(W.p, W.rows, W.cols, W.ld, Q.p, Q.ld, static_cast<uint8_t*>(S.p), S.ld, s); });
   NATIVE_END
@@ -382,13 +400,16 @@ NATIVE(linear_fp8) {
   NATIVE_ARGS(linear_fp8, 8);
   A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(5);
-  A.want_bytes(0, 1);
-  A.want_bytes(2, 2);
-  A.want_bytes(5, 2);
+  A.want_fp8(0, BSP_FP8_E4M3);
+  A.want_bf16(2);
+  A.want_bf16(5);
   A.want_shape(X, X.rows, W.cols);
   A.want_shape(Y, X.rows, W.rows);
   const void* bias = A.ptr(3);
-  if (bias != nullptr) A.want_values(3, W.rows, 2);
+  if (bias != nullptr) {
+    A.want_values(3, W.rows);
+    A.want_bf16(3);
+  }
   const int act = A.i32(4);
   void* ws = A.ptr(6);
   const size_t wsb = A.bytes(6);
@@ -405,14 +426,17 @@ NATIVE(linear_fp8_quantized) {
   A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), X = A.matrix(2), Y = A.matrix(7);
   const Matrix XS = A.scales(3, X.rows, blocks(X.cols));
-  A.want_bytes(0, 1);
-  A.want_bytes(2, 1);
-  A.want_bytes(7, 2);
+  const int fmt = A.i32(4), act = A.i32(6);
+  A.want_fp8(0, BSP_FP8_E4M3);
+  A.want_fp8(2, fmt);
+  A.want_bf16(7);
   A.want_shape(X, X.rows, W.cols);
   A.want_shape(Y, X.rows, W.rows);
-  const int fmt = A.i32(4), act = A.i32(6);
   const void* bias = A.ptr(5);
-  if (bias != nullptr) A.want_values(5, W.rows, 2);
+  if (bias != nullptr) {
+    A.want_values(5, W.rows);
+    A.want_bf16(5);
+  }
   void* s = A.stream(8);
   return status_of([&] {
     return bsp_linear_fp8_quantized(W.p, W.ld, static_cast<uint8_t*>(WS.p), WS.ld, W.rows, W.cols, X.p, X.ld, static_cast<uint8_t*>(XS.p), XS.ld, fmt,
@@ -427,12 +451,12 @@ NATIVE(linear_fp8_backward_input) {
   A.one_device();
   const Matrix W = A.matrix(0), WS = A.scales(1, blocks(W.rows), blocks(W.cols)), dY = A.matrix(2), dX = A.matrix(5);
   const Matrix dYS = A.scales(3, dY.rows, blocks(dY.cols));
-  A.want_bytes(0, 1);
-  A.want_bytes(2, 1);
-  A.want_bytes(5, 2);
+  const int fmt = A.i32(4);
+  A.want_fp8(0, BSP_FP8_E4M3);
+  A.want_fp8(2, fmt);
+  A.want_bf16(5);
   A.want_shape(dY, dY.rows, W.rows);
   A.want_shape(dX, dY.rows, W.cols);
-  const int fmt = A.i32(4);
   void* s = A.stream(6);
   return status_of([&] {
     return bsp_linear_fp8_backward_input(W.p, W.ld, static_cast<uint8_t*>(WS.p), WS.ld, W.rows, W.cols, dY.p, dY.ld, static_cast<uint8_t*>(dYS.p), dYS.ld,
@@ -447,14 +471,17 @@ NATIVE(linear_fp8_backward_weight) {
   A.one_device();
   const Matrix dY = A.matrix(0), dYS = A.scales(1, blocks(dY.rows), dY.cols), X = A.matrix(3), XS = A.scales(4, blocks(X.rows), X.cols);
   const Matrix dW = A.matrix(8);
-  A.want_bytes(0, 1);
-  A.want_bytes(3, 1);
-  A.want_bytes(8, 2);
+  const int fmt_dy = A.i32(2), fmt_x = A.i32(5), block = A.i32(6);
+  A.want_fp8(0, fmt_dy);
+  A.want_fp8(3, fmt_x);
+  A.want_bf16(8);
   A.want_shape(X, dY.rows, X.cols);
   A.want_shape(dW, dY.cols, X.cols);
-  const int fmt_dy = A.i32(2), fmt_x = A.i32(5), block = A.i32(6);
   const uint8_t* keep = A.ptr<uint8_t>(7);
-  if (keep != nullptr && block > 0) A.want_values(7, static_cast<long long>(dY.cols / block) * X.cols, 1);
+  if (keep != nullptr && block > 0) {
+    A.want_values(7, static_cast<long long>(dY.cols / block) * X.cols);
+    A.want_flags(7);
+  }
   void* s = A.stream(9);
   return status_of([&] {
     return bsp_linear_fp8_backward_weight(dY.p, dY.ld, static_cast<uint8_t*>(dYS.p), dYS.ld, fmt_dy, X.p, X.ld, static_cast<uint8_t*>(XS.p), XS.ld, fmt_x,
@@ -473,8 +500,14 @@ NATIVE(masked_adam_step_batched) {
   const uint32_t seed = static_cast<uint32_t>(A.integer(6));
   const float* scale = A.ptr<float>(7);
   const int* step_dev = A.ptr<int>(8);
-  if (scale != nullptr) A.want_values(7, 1, 4);
-  if (step_dev != nullptr) A.want_values(8, 1, 4);
+  if (scale != nullptr) {
+    A.want_values(7, 1);
+    A.want_type(7, {Args::Type::Float});
+  }
+  if (step_dev != nullptr) {
+    A.want_values(8, 1);
+    A.want_type(8, {Args::Type::Int});
+  }
   void* s = A.stream(9);
   return status_of([&] { return bsp_masked_adam_step_batched(jobs, n, b1, b2, eps, step, seed, scale, step_dev, s); });
   NATIVE_END
