@@ -460,9 +460,11 @@ class AdamJob:
 
 
 def make_adam_job_array(jobs):
-    """The host descriptor array for bsp_masked_adam_step_batched; build it once and reuse it while the tensors stay."""
+    """The host descriptor array for bsp_masked_adam_step_batched; build it once and reuse it: it holds addresses, and the tensors with
+    them.  Its entries have the fields of bsp_adam_job; lr and weight_decay may be set between calls (arr[i].lr = ...)."""
     arr = (_AdamJob * len(jobs))()
     arr.device = jobs[0].W.device.index if jobs else None
+    arr.tensors = [(j.W, j.grad, j.m, j.v, j.m_scale, j.v_scale, j.keep, j.W_bf16) for j in jobs]
     for a, j in zip(arr, jobs):
         shape = tuple(j.W.shape)
         for t in (j.W, j.grad, j.m, j.v, j.m_scale, j.v_scale, j.keep, j.W_bf16):

@@ -83,3 +83,35 @@ def test_types_of_the_linear_layer(name):
                 else:
                     call(**changed)
     torch.cuda.synchronize()
+
+
+def test_descriptors_hold_their_tensors(monkeypatch):
+    """An array that is used again must not name memory that has been given back: a gradient that was converted in place of the argument
+    lives as long as the array."""
+    import weakref
+
+    from paper_2009_08065_b200 import binding
+    monkeypatch.setattr(binding, "_ptr", lambda t: None if t is None else t.data_ptr())
+    job = adam_job(W_bf16=torch.bfloat16)
+    job.keep = torch.ones(4, 16, dtype=U8)
+    job.grad = torch.ones(4, 16).to(torch.bfloat16)
+    fields = ("W", "grad", "m", "v", "m_scale", "v_scale", "keep", "W_bf16")
+    refs = [weakref.ref(getattr(job, f)) for f in fields]
+    arr = bsp.make_adam_job_array([job])
+    addresses = [getattr(job, f).data_ptr() for f in fields]
+    del job
+    assert all(r() is not None for r in refs)
+    assert [getattr(arr[0], f) for f in fields] == addresses
+    del arr
+    assert all(r() is None for r in refs)
+
+
+@pytest.mark.gpu
+def test_learning_rate_between_calls():
+    job = adam_job(DEV)
+    job.W.fill_(1.0)
+    job.grad.fill_(1.0)
+    arr = bsp.make_adam_job_array([job])
+    arr[0].lr = 0.25
+    bsp.bsp_masked_adam_step_batched(arr, 0.9, 0.999, 1e-8, 1)
+    assert (job.W.cpu() - 0.75).abs().max() < 1e-6                      # (a first step of a constant gradient is lr)
