@@ -177,7 +177,10 @@ def _check(status: int, where: str) -> None:
 def _ld(t: torch.Tensor) -> int:
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError("expected a 2-D tensor with unit inner stride")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if max(ld, *t.shape) > 0x7FFFFFFF:                       # (ctypes and the structures' fields would cut it off without a word)
+        raise ValueError("a size or a row's distance beyond 2^31 - 1")
+    return ld
 
 
 def _per_group_shape(rows: int, cols: int, block: int, orient: int) -> Tuple[int, int]:

@@ -15,6 +15,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <algorithm>
+#include <climits>
 #include <initializer_list>
 
 #include "bsp.h"
@@ -48,6 +49,7 @@ class Args {
     const at::Tensor& t = tensor(i);
     TORCH_CHECK_VALUE(t.dim() == 2 && t.stride(1) == 1, "expected a 2-D tensor with unit inner stride");
     const int64_t ld = t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
+    TORCH_CHECK_VALUE(std::max({t.size(0), t.size(1), ld}) <= INT_MAX, "a size or a row's distance beyond 2^31 - 1");
     return Matrix{t.data_ptr(), static_cast<int>(t.size(0)), static_cast<int>(t.size(1)), static_cast<int>(ld)};
   }
   // Every tensor on the current device, whose stream the call goes to.
@@ -97,7 +99,11 @@ class Args {
     if (v == -1 && PyErr_Occurred()) throw python_error();
     return v;
   }
-  int i32(int i) const { return static_cast<int>(integer(i)); }
+  int i32(int i) const {
+    const long long v = integer(i);
+    TORCH_CHECK_VALUE(v >= INT_MIN && v <= INT_MAX, "a number beyond 32 bits");
+    return static_cast<int>(v);
+  }
   double real(int i) const {
     const double v = PyFloat_AsDouble(a_[i]);
     if (v == -1.0 && PyErr_Occurred()) throw python_error();
