@@ -74,3 +74,31 @@ def test_nothing_is_read_ahead_of_the_wait(path):
     for m in firsts:
         role = src[:m.start()].rindex("if (warp ==")
         assert "pdl_wait();" in src[role:m.start()], f"{path}: {m.group(0)}"
+
+
+def kernels(path):
+    """name, parameters and body of every kernel of a file, whatever its parameters."""
+    src = source(path)
+    for m in re.finditer(r"__global__", src):
+        name = re.compile(r"(\w+)\s*\((?!\w*Threads|\d|32 \*)").search(src, src.index("\n", m.start()) if "__launch_bounds__" in src[m.start():src.index("\n", m.start())] else m.start())
+        end = closing(src, name.end(0) - 1 if src[name.end(0) - 1] == "(" else src.index("(", name.start()))
+        body = src.index("{", end)
+        yield name.group(1), src[name.end():end], src[body:closing(src, body, "{}") + 1]
+
+
+def test_every_kernel_of_the_8_bit_files_is_looked_at():
+    """The rules of test_launch_overlap.py for the kernels of the 8-bit calls, whose parameters are structures of their own."""
+    found = {}
+    for path in [os.path.basename(p) for p in SOURCES if "fp8" in p or "adam_batched" in p]:
+        for name, params, body in kernels(path):
+            found[name] = body
+            assert "pdl_wait()" in body and "pdl_launch_dependents()" in body, f"{path}: {name}"
+            assert "__ldg(" not in body and not re.search(r"const\s+\w+\s*\*\s*__restrict__", params), f"{path}: {name}"
+            assert body.index("pdl_wait()") < body.index("pdl_launch_dependents()"), f"{path}: {name} signals ahead of its wait"
+            if "tcgen05.alloc" in body:
+                assert body.index("tcgen05.alloc") < body.index("pdl_launch_dependents()"), f"{path}: {name}"
+    assert set(found) == {"quantize_kernel", "quantize_both_kernel", "column_sums_kernel", "linear_few_kernel", "product_any_kernel", "gemm_fp8_pair_kernel",
+                          "gemm_fp8_split_kernel", "adam_batched_kernel", "adam_stream8_kernel", "adam_batched8_kernel"}
+    assert {n for n, body in found.items() if "tcgen05.alloc" in body} == {"gemm_fp8_pair_kernel", "gemm_fp8_split_kernel"}
+    for header in glob.glob(os.path.join(CSRC, "*.cuh")):
+        assert "__ldg(" not in source(header), header
