@@ -437,11 +437,12 @@ def bsp_linear_fp8_backward_weight(dYq: torch.Tensor, dYS: torch.Tensor, fmt_dy:
            "bsp_linear_fp8_backward_weight")
 
 
-# Element types that are taken: the one that is meant, or whole numbers of its size as its bits.
-_FLOAT32 = (torch.float32,)
-_BF16 = (torch.bfloat16, torch.int16, torch.uint16)
-_E4M3, _E5M2 = (torch.float8_e4m3fn, torch.uint8, torch.int8), (torch.float8_e5m2, torch.uint8, torch.int8)
-_SCALE, _FLAGS = (torch.uint8, torch.int8, torch.float8_e8m0fnu), (torch.uint8, torch.int8, torch.bool)
+# Element types that are taken: the one that is meant, or whole numbers of its size as its bits.  By the place in a descriptor's tensors.
+_TENSORS = ("W", "grad", "m", "v", "m_scale", "v_scale", "keep", "W_bf16")
+_BF16, _BYTES = {torch.bfloat16, torch.int16, torch.uint16}, {torch.uint8, torch.int8}
+_TYPES8 = ({torch.float32}, {torch.float32} | _BF16, {torch.float8_e4m3fn} | _BYTES, {torch.float8_e5m2} | _BYTES, {torch.float8_e8m0fnu} | _BYTES,
+           {torch.float8_e8m0fnu} | _BYTES, {torch.bool} | _BYTES, _BF16)
+_TYPES32 = _TYPES8[:2] + ({torch.float32}, {torch.float32}) + _TYPES8[4:]
 
 
 @dataclass
@@ -468,34 +469,38 @@ def make_adam_job_array(jobs):
     arr = (_AdamJob * len(jobs))()
     arr.device = jobs[0].W.device.index if jobs else None
     arr.tensors = [(j.W, j.grad, j.m, j.v, j.m_scale, j.v_scale, j.keep, j.W_bf16) for j in jobs]
-    for a, j in zip(arr, jobs):
-        shape = tuple(j.W.shape)
-        for t in (j.W, j.grad, j.m, j.v, j.m_scale, j.v_scale, j.keep, j.W_bf16):
-            if t is not None and t.device != j.W.device or j.W.device.index != arr.device:
+    for a, j, tensors in zip(arr, jobs, arr.tensors):
+        W, grad, m, v, m_scale, v_scale, keep, W_bf16 = tensors
+        shape, device = W.shape, W.device
+        rows, cols = shape
+        for t in tensors:
+            if t is not None and t.device != device:
                 raise ValueError("the tensors of a call are on different devices")
-        for t in (j.grad, j.m, j.v, j.W_bf16):
-            if t is not None and tuple(t.shape) != shape:
-                raise ValueError(f"tensors of one job have shapes {shape} and {tuple(t.shape)}")
-        moments = (_FLOAT32, _FLOAT32) if j.m.dtype in _FLOAT32 else (_E4M3, _E5M2)
-        for name, t, types in (("W", j.W, _FLOAT32), ("grad", j.grad, _FLOAT32 + _BF16), ("m", j.m, moments[0]), ("v", j.v, moments[1]),
-                               ("W_bf16", j.W_bf16, _BF16), ("m_scale", j.m_scale, _SCALE), ("v_scale", j.v_scale, _SCALE)):
-            if t is not None and t.dtype not in types:
-                raise ValueError(f"unexpected element type of {name}: {t.dtype}")
-        if _ld(j.m) != _ld(j.v):
+        if device.index != arr.device:
+            raise ValueError("the tensors of a call are on different devices")
+        for t in (grad, m, v, W_bf16):
+            if t is not None and t.shape != shape:
+                raise ValueError(f"tensors of one job have shapes {tuple(shape)} and {tuple(t.shape)}")
+        types = _TYPES32 if m.dtype == torch.float32 else _TYPES8
+        for i, t in enumerate(tensors):
+            if t is not None and t.dtype not in types[i]:
+                raise ValueError(f"{_TENSORS[i]} is of an unexpected element type, {t.dtype}")
+        ldm = _ld(m)
+        if ldm != _ld(v):
             raise ValueError("m and v have different leading dimensions")
-        scales = (shape[0], (shape[1] + 127) // 128)
-        for t in (j.m_scale, j.v_scale):
-            if t is not None and (tuple(t.shape) != scales or not t.is_contiguous()):
+        scales = (rows, (cols + 127) // 128)
+        for t in (m_scale, v_scale):
+            if t is not None and (t.shape != scales or not t.is_contiguous()):
                 raise ValueError(f"scales are contiguous bytes of shape {scales}")
-        if j.keep is not None and (j.keep.numel() * j.block != shape[0] * shape[1] or not j.keep.is_contiguous() or j.keep.dtype not in _FLAGS):
-            raise ValueError(f"keep is a contiguous byte for each group of {j.block} of {shape[0]} x {shape[1]} weights")
-        a.W, a.rows, a.cols, a.ldw = _ptr(j.W), shape[0], shape[1], _ld(j.W)
-        a.grad, a.ldg, a.grad_type = _ptr(j.grad), _ld(j.grad), GRAD_BF16 if j.grad.element_size() == 2 else GRAD_F32
-        a.m, a.v, a.ldm, a.state_bits = _ptr(j.m), _ptr(j.v), _ld(j.m), 8 * j.m.element_size()
-        a.m_scale, a.v_scale = _ptr(j.m_scale), _ptr(j.v_scale)
-        a.keep, a.block, a.orient = _ptr(j.keep), j.block, j.orient
+        if keep is not None and (keep.numel() * j.block != rows * cols or not keep.is_contiguous()):
+            raise ValueError(f"keep is a contiguous byte for each group of {j.block} of {rows} x {cols} weights")
+        a.W, a.rows, a.cols, a.ldw = _ptr(W), rows, cols, _ld(W)
+        a.grad, a.ldg, a.grad_type = _ptr(grad), _ld(grad), GRAD_F32 if grad.dtype == torch.float32 else GRAD_BF16
+        a.m, a.v, a.ldm, a.state_bits = _ptr(m), _ptr(v), ldm, 32 if types is _TYPES32 else 8
+        a.m_scale, a.v_scale = _ptr(m_scale), _ptr(v_scale)
+        a.keep, a.block, a.orient = _ptr(keep), j.block, j.orient
         a.lr, a.weight_decay = j.lr, j.weight_decay
-        a.W_bf16, a.ldb = _ptr(j.W_bf16), 0 if j.W_bf16 is None else _ld(j.W_bf16)
+        a.W_bf16, a.ldb = _ptr(W_bf16), 0 if W_bf16 is None else _ld(W_bf16)
     return arr
 
 
