@@ -517,7 +517,8 @@ int bsp_linear_tune(const bsp_linear_call* call, int reps, int* best_route, floa
  * Xq [tokens, k_in], XS [ceil(tokens / 128), k_in]); keep and block as in bsp_linear_backward_weight; dW bf16 [n_out, k_in].
  *
  * Products of 8-bit values are exact; they are added in float32 and the result is rounded to bf16 once.  8-bit matrices whose
- * rows begin at multiples of 16 bytes go through the tensor cores, others through a slower CUDA-core kernel with the same semantics.
+ * rows begin at multiples of 16 bytes go through the tensor cores, others through a CUDA-core kernel with the same semantics that takes 15 to 25
+ * times as long: give 8-bit matrices leading dimensions of a multiple of 16.
  * Outputs may have any alignment; they are stored fastest where they are 16-byte aligned with rows and leading dimensions of a
  * multiple of 8.  Bounded waits as bsp_linear_planned: check bsp_linear_status.
  * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE (leading dimension too small, block does not divide n_out), BSP_ERR_WORKSPACE,
@@ -555,7 +556,8 @@ int bsp_linear_fp8_backward_weight(const void* dYq, int ldy, const uint8_t* dYS,
  *     gives the same bits.  A positive v is never rounded to zero.  A block whose new moments hold an infinity or a NaN at a kept
  *     place becomes NaN; at a pruned place where either of the two is not finite, both begin again at zero.
  * grad_scale: device float that multiplies every gradient (clipping), or NULL.  step >= 1; if step_dev is not NULL the step is read from there
- * instead (it has to be at least 1 when the call runs), so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step.
+ * instead (it has to be at least 1 when the call runs), so that a captured graph can be replayed with the next one.  beta1, beta2, eps as in bsp_masked_adam_step; with 8-bit moments an eps
+ * above zero and below 2^-126 counts as 2^-126.
  * Any shape and alignment; 16-byte accesses where pointers and leading dimensions allow them.  No two jobs may share memory that either writes.
  * Bounded waits (8-bit moments) as bsp_linear_planned: check bsp_linear_status.
  * Errors: BSP_ERR_ARG, BSP_ERR_SHAPE, BSP_ERR_UNSUPPORTED (more than 2^31 - 512 rows or columns, or 2^41 weights); all jobs are

@@ -1,11 +1,11 @@
 // bsp_fp8_quantize, bsp_fp8_quantize_weight: bf16 matrices to 8 bits with a scale for each block of 128.
 //
-// A CTA holds a tile of 128 x 128 in registers (256 threads, 4 rows x 16 columns each, all loads in flight) and writes from
-// there whichever forms are asked for: along the rows (a scale for each 128 columns of a row: the operand of a product that
+// A CTA holds a tile of 128 x 128 in registers (256 threads, 4 rows x 16 columns each, all loads in flight; along the rows alone, beyond 64 of them, 64 x 128
+// and 128 threads) and writes from there whichever forms are asked for: along the rows (a scale for each 128 columns of a row: the operand of a product that
 // sums over the columns), along the columns (a scale for each 128 rows of a column: the operand of a product that sums over the
 // rows), or one scale for the tile (weights: the same 8-bit values then serve both products).  A training step needs the first
 // two of the same matrix, and for the output gradient its column sums (the bias gradient) too: one pass over the matrix.
-// HBM-bound: 2 bytes read and 1 or 2 written per value.
+// 2 bytes read and 1 or 2 written per value: along the rows HBM binds, along both directions half of the time goes at barriers (see there).
 #include <algorithm>
 
 #include "bsp_fp8.cuh"

@@ -93,7 +93,7 @@ __device__ __forceinline__ void finish_piece(const Fp8Params& P, uint32_t (&v)[3
 // Every CTA holds the scales of its own rows of A and of all rows of B of the tile.
 // Roles per CTA: warps 0 and 11 TMA producers of A and B (completion is counted on the leader's mbarrier), warp 10 the scales, warp 1 of
 // the LEADER issues the MMAs and commits to both CTAs' barriers, warps 2 to 9 epilogue of the CTA's own 128 rows: two groups of four.  (With GELU
-// the issue of its arithmetic binds, 4096 x 4096 x 1024 18.3 us without and 22.3 with it, not the number of warps: with three groups the same.)
+// the epilogue binds, 4096 x 4096 x 1024 18.3 us without and 22.3 with it, by the latency of its chain: 38 % of issue slots; with three groups the same.)
 // 384 threads of up to 140 registers leave room on the SM for a CTA of the quantiser (bsp_fp8_quantize.cu), which therefore starts
 // while these run, and these while it runs.  No TMA multicast is used.  All mbarrier waits are bounded.
 constexpr int kFp8Threads = 384;

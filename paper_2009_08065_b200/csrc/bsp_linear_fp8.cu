@@ -1,5 +1,5 @@
-// The linear layer in 8-bit floating point: entry points, the kernel for few tokens, and the plain kernel for operands that
-// the tensor core's copies cannot fetch.
+// The linear layer in 8-bit floating point: entry points, the choice of a kernel, and the plain kernel for operands that the tensor core's
+// copies cannot fetch.
 #include "bsp_fp8.cuh"
 #include "bsp_fp8_gemm.cuh"
 
@@ -10,7 +10,8 @@ namespace {
 
 // ------------------------------------------------------------------------------------------ any alignment
 // 64 x 64 outputs per CTA, 4 x 4 per thread, 32 of the contraction at a time from shared memory, values already multiplied by
-// their scales (powers of two: exact).  For operands whose rows do not begin at multiples of 16 bytes.
+// their scales (powers of two: exact).  For operands whose rows do not begin at multiples of 16 bytes.  Bound by CUDA-core multiply-adds and byte loads:
+// 1003 tokens, 920 -> 2128 282 us, 11 with padded rows on tensor cores.
 constexpr int kAnyTile = 64, kAnyDepth = 32;
 
 struct AnyArgs {
