@@ -33,7 +33,7 @@ def tensors(shapes, grad16, mixed):
     return sets
 
 
-# Chunks of 2048 weights; three CTAs of each of 148 SMs take one at a time: 4096 of the large tensor are nine rounds.  Small and ragged
+# Chunks of 2048 weights; three CTAs of each of 148 SMs take one at a time: 4096 of the large tensor are nine turns.  Small and ragged
 # tensors between large ones, so that a CTA goes from one tensor to another, and past several, between two of its chunks.
 LARGE = [(2048, 4096, 16)]
 MIXED = [(1024, 1024, 16), (1, 1024, 0), (3, 136, 3), (1, 8, 0), (1100, 920, 4), (1, 920, 0), (2048, 1024, 0), (1, 4096, 0), (5, 200, 1), (920, 3680, 8), (1, 3680, 0), (700, 1288, 1)]
@@ -41,7 +41,7 @@ MIXED = [(1024, 1024, 16), (1, 1024, 0), (3, 136, 3), (1, 8, 0), (1100, 920, 4),
 
 @pytest.mark.parametrize("shapes,grad16,mixed", [(LARGE, True, False), (LARGE, False, False), (MIXED, True, False), (MIXED, False, True), (MIXED * 9, True, True)],
                          ids=["large bf16", "large float32", "small and large", "both gradients", "two launches"])
-def test_many_rounds(shapes, grad16, mixed):
+def test_many_chunks(shapes, grad16, mixed):
     dense, gaps = tensors(shapes, grad16, mixed)
     a, b = bsp.make_adam_job_array(dense), bsp.make_adam_job_array(gaps)
     scale = torch.full((1,), 0.5, dtype=torch.float32, device=DEV)
